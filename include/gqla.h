@@ -268,6 +268,91 @@ gqla_status gqla_decode_gqa_fp8(const gqla_dims* dims, int32_t B, int32_t s_q, f
                                 const int64_t* seq_start, const int32_t* seqlens, float* o_part, float* lse_part,
                                 int32_t* status_word, void* stream);
 
+/* ---- Appending rows to the cache, with the position rotation applied on the way ----
+ * The paper writes k^R and q^R as they enter the scores, rotated; these calls take them as they leave their projections.
+ * New rows come packed, sequence 0 first: row i (new_start[b] <= i < new_start[b+1]) of sequence b goes to position
+ * t = seqlens[b] - new_start[b+1] + i, so that seqlens counts the new rows already and a step of s_q tokens has
+ * new_start = 0, s_q, 2 s_q, ..; a prompt has as many rows as its sequence.  Rows at negative positions are skipped.
+ * new_start int32 [B+1] (device, ascending, new_start[0] = 0, new_start[B] = n_new), seqlens int32 [B] (device).
+ *   rope  fp32 [rope_rows, d_r]: row t holds the cosines of position t's d_r / 2 angles, then their sines.
+ *   style GQLA_ROPE_PAIRS turns the columns (2 i, 2 i + 1), GQLA_ROPE_HALVES (i, i + d_r / 2), by angle i:
+ *         (a, b) -> (a cos - b sin, a sin + b cos), in fp32, rounded once to what is stored.
+ *   q_r   [n_new, h_q, d_r] (strides in elements, last dimension contiguous) or NULL: the same rows' queries, rotated
+ *         into q_out (strides of its own; q_out == q_r with the same strides turns them in place).
+ * A position of rope_rows or more, a block-table column of max_pages or more, or a row or page outside the cache is left
+ * out, and GQLA_ERR_SHAPE | (1 << 8) (rotation table) or GQLA_ERR_SHAPE | (2 << 8) goes to *status_word (may be NULL).
+ * Nothing but the new rows is written (and with E4M3 pages the older rows of a page whose scale grows).  The pages that
+ * get rows belong to one sequence each; d_r must be even. */
+typedef enum { GQLA_ROPE_PAIRS = 0, GQLA_ROPE_HALVES = 1 } gqla_rope_style;
+
+/* Latent cache in the storage type: cache row = [c ; rotated k_r].  c [n_new, r_kv] and k_r [n_new, d_r] with row strides.
+ * Packed (seq_start, block_table NULL) or paged (block_table, seq_start NULL) as for the decode calls; one of the two. */
+gqla_status gqla_append_rope(const gqla_dims* dims, gqla_dtype dtype, int32_t B, int64_t n_new, const int32_t* new_start,
+                             const int32_t* seqlens, const void* c, int64_t c_row_stride, const void* k_r,
+                             int64_t k_r_row_stride, const float* rope, int32_t rope_rows, gqla_rope_style style,
+                             const void* q_r, int64_t q_row_stride, int64_t q_head_stride, void* q_out,
+                             int64_t q_out_row_stride, int64_t q_out_head_stride, void* cache, int64_t cache_row_stride,
+                             int64_t cache_rows, const int64_t* seq_start, const int32_t* block_table, int32_t max_pages,
+                             int32_t page_size, int32_t* status_word, void* stream);
+
+/* E4M3 pages with a scale per page: a stored value is code * page_scale[page].  The scale is a power of two, the smallest
+ * 2^e (e >= -40) with |x| <= 448 * 2^e for every finite x of the page's rows so far, and is set here: the first rows of
+ * a page (those at its position 0) start it anew, later ones may raise it, in which case the page's older codes are coded
+ * again under the larger scale (exact but for what falls below 2^-6 of it, which keeps a multiple of 2^-9).  Values are
+ * rounded once, from fp32, to the nearest code, ties to even; infinities saturate, NaN stays NaN.
+ *   cache8 [cache_rows, r_kv + d_r] codes (row stride in bytes), page_scale fp32 [cache_rows / page_size]. */
+gqla_status gqla_append_rope_fp8(const gqla_dims* dims, gqla_dtype dtype, int32_t B, int64_t n_new, const int32_t* new_start,
+                                 const int32_t* seqlens, const void* c, int64_t c_row_stride, const void* k_r,
+                                 int64_t k_r_row_stride, const float* rope, int32_t rope_rows, gqla_rope_style style,
+                                 const void* q_r, int64_t q_row_stride, int64_t q_head_stride, void* q_out,
+                                 int64_t q_out_row_stride, int64_t q_out_head_stride, uint8_t* cache8,
+                                 int64_t cache_row_stride, int64_t cache_rows, float* page_scale,
+                                 const int32_t* block_table, int32_t max_pages, int32_t page_size, int32_t* status_word,
+                                 void* stream);
+
+/* The GQA path's planes with a scale per page and group: k_c, v [n_new, g, d_h] dense (the new rows, expanded, e.g. by
+ * gqla_expand_cache on the new latent rows) -> k_c8, v8 [n_rows, g, d_h] with k_scale, v_scale fp32 [n_rows / page_size, g];
+ * k_r, rotated -> k_r8 [n_rows, d_r] (row stride in bytes) with r_scale fp32 [n_rows / page_size].  Scales and codes as for
+ * gqla_append_rope_fp8, each head of a page by itself. */
+gqla_status gqla_append_planes_fp8(const gqla_dims* dims, gqla_dtype dtype, int32_t B, int64_t n_new,
+                                   const int32_t* new_start, const int32_t* seqlens, const void* k_c, const void* v,
+                                   const void* k_r, int64_t k_r_row_stride, const float* rope, int32_t rope_rows,
+                                   gqla_rope_style style, const void* q_r, int64_t q_row_stride, int64_t q_head_stride,
+                                   void* q_out, int64_t q_out_row_stride, int64_t q_out_head_stride, uint8_t* k_c8,
+                                   uint8_t* v8, uint8_t* k_r8, int64_t k_r8_row_stride, int64_t n_rows, float* k_scale,
+                                   float* v_scale, float* r_scale, const int32_t* block_table, int32_t max_pages,
+                                   int32_t page_size, int32_t* status_word, void* stream);
+
+/* ---- Attention over E4M3 pages with a scale per page and head ----
+ * The decode calls of both paths over what the two calls above write (any positive finite scales of at least 2^-60 will do):
+ *   absorb path  x_t = scale s_t (q_hat . k8_t),                            o = sum_t p_t s_t k8_t[:r_kv] / sum_t p_t
+ *   GQA path     x_t = scale (k_s (q_C . k_c8_t) + r_s (q_R . k_r8_t)),     o = sum_t p_t v_s v8_t / sum_t p_t
+ * with the scales of token t's page (and the head's group).  Queries come in `dtype` (q_hat [B, s_q, h_q, r_kv+d_r], q
+ * [B, s_q, h_q, d_h+d_r]) and are not rounded further than bf16: the tensor-core kernels multiply two E4M3 terms of
+ * each query and each probability, which keep as much (a query element below 2^-15 of its row's largest keeps an
+ * absolute error of 2^-19 of that one).  Rows of a sequence's last page behind its end may hold anything.
+ * Block table, lengths, splits (num_splits >= 1 fixed plan, <= -2 balanced), partials and status word as for
+ * gqla_decode_absorb_paged / gqla_decode_gqa_paged; with `out` not NULL ([B, s_q, h_q, r_kv] or [.., d_h] of `dtype`) the call
+ * also merges the partials as gqla_combine_splits does (lse fp32 [B, s_q, h_q] or NULL, NULL without out).  Tensor-core kernels:
+ * bf16 queries, d_r = 64, r_kv = 512 (absorb) or d_h = 128 (GQA), pages of a multiple of 16 rows, any number of query rows;
+ * everything else runs on a generic kernel (values up to 512 wide), where a page outside the cache is left out and reported
+ * in the status word as above. */
+gqla_status gqla_decode_absorb_fp8_paged(const gqla_dims* dims, gqla_dtype dtype, int32_t B, int32_t s_q, float scale,
+                                         int32_t num_splits, const void* q_hat, const uint8_t* cache8,
+                                         int64_t cache_row_stride, int64_t cache_rows, const float* page_scale,
+                                         const int32_t* block_table, int32_t max_pages, int32_t page_size,
+                                         const int32_t* seqlens, float* o_part, float* lse_part, void* out, float* lse,
+                                         int32_t* status_word, void* stream);
+gqla_status gqla_decode_gqa_fp8_paged(const gqla_dims* dims, gqla_dtype dtype, int32_t B, int32_t s_q, float scale,
+                                      int32_t num_splits, const void* q, const uint8_t* k_c8, const uint8_t* v8,
+                                      const uint8_t* k_r8, int64_t k_r8_row_stride, int64_t n_rows, const float* k_scale,
+                                      const float* v_scale, const float* r_scale, const int32_t* block_table,
+                                      int32_t max_pages, int32_t page_size, const int32_t* seqlens, float* o_part,
+                                      float* lse_part, void* out, float* lse, int32_t* status_word, void* stream);
+/* Workers a balanced call of the two is cut for on the CURRENT device (path: 0 = absorb, 1 = GQA), to be used with
+ * gqla_balanced_plan; 0 where the fixed plan is used instead, -1 on error. */
+int32_t gqla_fp8_paged_workers(const gqla_dims* dims, gqla_dtype dtype, int32_t s_q, int32_t page_size, int32_t path);
+
 /* Log-sum-exp merge of split partials (split-KV is not in the paper; it is the flash-decoding
  * reduction of the same softmax):  M = max_k lse_k, w_k = exp(lse_k - M),
  *   out = sum_k w_k o_k / sum_k w_k,   lse = M + ln sum_k w_k;  all splits empty -> out = 0, lse = -inf.

@@ -483,6 +483,82 @@ def brute_force_path(dims, q_c, q_r, w_uk, w_uv, cache, seq_start, seqlens, s_q,
 
 
 # --------------------------------------------------------------------------
+# appending to the cache with the position rotation; E4M3 pages with a scale per page and head
+# --------------------------------------------------------------------------
+
+SMALLEST_SCALE_EXP = -40
+
+
+def rope_turn(x: np.ndarray, pos, table: np.ndarray, style: str) -> np.ndarray:
+    """Rows x [n, ..., d] at positions pos [n]: pair i of a row, (2i, 2i+1) with style "pairs" and (i, i + d/2) with
+    "halves", turned by the angle whose cosine is table[pos, i] and whose sine is table[pos, d/2 + i]."""
+    x = np.asarray(x, dtype=np.float64)
+    out = np.empty_like(x)
+    half = x.shape[-1] // 2
+    for n, t in enumerate(pos):
+        for i in range(half):
+            a, b = (2 * i, 2 * i + 1) if style == "pairs" else (i, i + half)
+            c, s = float(table[t, i]), float(table[t, half + i])
+            out[n, ..., a] = x[n, ..., a] * c - x[n, ..., b] * s
+            out[n, ..., b] = x[n, ..., a] * s + x[n, ..., b] * c
+    return out
+
+
+def new_row_places(new_start, seqlens):
+    """(sequence, position) of every new row; positions may be negative (the row is skipped)."""
+    out = []
+    for b, T in enumerate(seqlens):
+        n = int(new_start[b + 1]) - int(new_start[b])
+        out += [(b, int(T) - n + i) for i in range(n)]
+    return out
+
+
+def pow2_scale(amax: float) -> float:
+    """The smallest 2^e, e >= SMALLEST_SCALE_EXP, with amax <= 448 * 2^e."""
+    e = SMALLEST_SCALE_EXP
+    while amax > E4M3_MAX * 2.0 ** e:
+        e += 1
+    return 2.0 ** e
+
+
+def append_pages_e4m3(rows, codes, scale, new_start, seqlens, block_table, page_size):
+    """New rows [n, heads, width] into codes [N, heads, width] with scale [pages, heads]; returns new copies.  Row after row:
+    a page's first row (position 0 of the page) starts its scale anew, and whenever a head's scale grows the rows that are
+    in the page already are coded again from the values that they stand for.  (A page's scale is that of its largest value;
+    within one call older rows are coded again once, so the rows of the call are coded only when all of them are known.)"""
+    rows = np.asarray(rows, dtype=np.float64)
+    codes, scale = codes.copy(), scale.astype(np.float64)
+    places = new_row_places(new_start, seqlens)
+    pages = {}
+    for i, (b, t) in enumerate(places):
+        if t >= 0:
+            pages.setdefault((b, t // page_size), []).append((i, t % page_size))
+    for (b, k), mine in pages.items():
+        page = int(block_table[b, k])
+        base, first = page * page_size, mine[0][1]
+        for h in range(codes.shape[1]):
+            vals = np.array([rows[i, h] for i, _ in mine])
+            finite = np.abs(vals[np.isfinite(vals)])
+            s = pow2_scale(float(finite.max()) if finite.size else 0.0)
+            if first > 0:
+                old = scale[page, h]
+                if old >= s:
+                    s = old
+                else:
+                    codes[base:base + first, h] = e4m3_encode(e4m3_decode(codes[base:base + first, h]) * (old / s))
+            scale[page, h] = s
+            for i, at in mine:
+                codes[base + at, h] = e4m3_encode(rows[i, h] / s)
+    return codes, scale.astype(np.float32)
+
+
+def page_values(codes, scale, page_size):
+    """What codes [N, heads, width] with scale [pages, heads] stand for."""
+    per_row = np.repeat(np.asarray(scale, dtype=np.float64), page_size, axis=0)
+    return e4m3_decode(codes) * per_row[:, :, None]
+
+
+# --------------------------------------------------------------------------
 # analytic accounting of Sec. 4.2 (Eqs. mqa-bytes-tok .. gqa-ai, Table "roofline")
 # --------------------------------------------------------------------------
 

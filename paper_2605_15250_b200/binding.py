@@ -18,6 +18,7 @@ LIB_PATH = os.environ.get("GQLA_LIB_PATH") or os.path.join(_PKG_DIR, "libgqla.so
 
 GQLA_BF16, GQLA_F32 = 0, 1
 POLICY_AUTO, POLICY_GENERIC = 0, 1
+ROPE_STYLES = {"pairs": 0, "halves": 1}
 
 
 class GqlaDims(ctypes.Structure):
@@ -80,6 +81,24 @@ _PROTOTYPES = {
     "gqla_decode_gqa_fp8": (c_int32, [c_void_p, c_int32, c_int32, c_float, c_int32, c_void_p, c_void_p, c_void_p, c_void_p,
                                       c_void_p, c_int64, c_int64, c_float, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
                                       c_void_p]),
+    "gqla_append_rope": (c_int32, [c_void_p, c_int32, c_int32, c_int64, c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_int64,
+                                   c_void_p, c_int32, c_int32, c_void_p, c_int64, c_int64, c_void_p, c_int64, c_int64, c_void_p,
+                                   c_int64, c_int64, c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_void_p]),
+    "gqla_append_rope_fp8": (c_int32, [c_void_p, c_int32, c_int32, c_int64, c_void_p, c_void_p, c_void_p, c_int64, c_void_p,
+                                       c_int64, c_void_p, c_int32, c_int32, c_void_p, c_int64, c_int64, c_void_p, c_int64,
+                                       c_int64, c_void_p, c_int64, c_int64, c_void_p, c_void_p, c_int32, c_int32, c_void_p,
+                                       c_void_p]),
+    "gqla_append_planes_fp8": (c_int32, [c_void_p, c_int32, c_int32, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                         c_int64, c_void_p, c_int32, c_int32, c_void_p, c_int64, c_int64, c_void_p, c_int64,
+                                         c_int64, c_void_p, c_void_p, c_void_p, c_int64, c_int64, c_void_p, c_void_p, c_void_p,
+                                         c_void_p, c_int32, c_int32, c_void_p, c_void_p]),
+    "gqla_decode_absorb_fp8_paged": (c_int32, [c_void_p, c_int32, c_int32, c_int32, c_float, c_int32, c_void_p, c_void_p, c_int64,
+                                               c_int64, c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_void_p,
+                                               c_void_p, c_void_p, c_void_p, c_void_p]),
+    "gqla_decode_gqa_fp8_paged": (c_int32, [c_void_p, c_int32, c_int32, c_int32, c_float, c_int32, c_void_p, c_void_p, c_void_p,
+                                            c_void_p, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_int32, c_int32,
+                                            c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
+    "gqla_fp8_paged_workers": (c_int32, [c_void_p, c_int32, c_int32, c_int32, c_int32]),
     "gqla_split_plan": (c_int32, [c_int32, c_int32, c_void_p, c_void_p]),
     "gqla_visible_limit": (c_int32, [c_int32, c_int32, c_int32]),
     "gqla_balanced_plan": (c_int32, [c_void_p, c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p]),
@@ -428,6 +447,196 @@ def gqla_decode_gqa_fp8(dims: GqlaDims, q8: torch.Tensor, q_scale: torch.Tensor,
                                      _ptr(v8), _ptr(k_r8), k_r8.stride(0), k_c8.shape[0], v_scale, _ptr(seq_start),
                                      _ptr(seqlens), _ptr(o_part), _ptr(lse_part), _ptr(status_word), _stream()),
            "gqla_decode_gqa_fp8")
+
+
+# ------------------------------------------------------------------ appending with rotation, E4M3 pages
+
+
+def _on_current_device(*ts: torch.Tensor | None) -> None:
+    """The calls below are issued on the current device's current stream: their tensors have to live there."""
+    here = torch.cuda.current_device()
+    for t in ts:
+        if t is not None and (not t.is_cuda or t.device.index != here):
+            raise GqlaError(f"expected a tensor on cuda:{here}, got one on {t.device}")
+
+
+def _shape(what: str, t: torch.Tensor, shape: tuple, dtype: torch.dtype) -> None:
+    if tuple(t.shape) != shape or t.dtype != dtype:
+        raise GqlaError(f"{what}: expected {dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
+
+
+def _rows(what: str, t: torch.Tensor, shape: tuple, dtype: torch.dtype) -> int:
+    """A tensor of rows: the last dimension contiguous, rows `stride` elements apart.  Returns the row stride."""
+    _shape(what, t, shape, dtype)
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise GqlaError(f"{what}: the last dimension has to be contiguous")
+    # the stride of a dimension of one element is arbitrary and never stepped by
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[-1] if t.dim() == 2 else t.shape[-1] * t.shape[-2])
+
+
+def _append_args(dims: GqlaDims, n: int, dtype: torch.dtype, k_r, new_start, seqlens, rope, style, q_r, q_out):
+    """(sequences, arguments from new_start and seqlens on) that the three append calls share."""
+    B = seqlens.shape[0]
+    if style not in ROPE_STYLES:
+        raise GqlaError(f"style is one of {sorted(ROPE_STYLES)}, got {style!r}")
+    _contig(new_start, seqlens, rope)
+    _shape("seqlens", seqlens, (B,), torch.int32)
+    _shape("new_start", new_start, (B + 1,), torch.int32)
+    _shape("rope", rope, (rope.shape[0], dims.d_r), torch.float32)
+    k_r_stride = _rows("k_r", k_r, (n, dims.d_r), dtype)
+    if (q_r is None) != (q_out is None):
+        raise GqlaError("q_r and q_out come together")
+    q = [None, 0, 0, None, 0, 0]
+    if q_r is not None:
+        q = []
+        for name, t in (("q_r", q_r), ("q_out", q_out)):
+            row = _rows(name, t, (n, dims.h_q, dims.d_r), dtype)
+            head = t.stride(1) if dims.h_q > 1 else max(t.stride(1), dims.d_r)
+            q += [_ptr(t), row, head]
+    return B, [_ptr(new_start), _ptr(seqlens)], [_ptr(k_r), k_r_stride, _ptr(rope), rope.shape[0], ROPE_STYLES[style], *q]
+
+
+def _pages(n_rows: int, block_table: torch.Tensor, page_size: int, B: int):
+    _contig(block_table)
+    if block_table.dtype != torch.int32 or block_table.dim() != 2 or block_table.shape[0] != B:
+        raise GqlaError(f"block_table: expected int32 [{B}, max_pages], got {block_table.dtype} {tuple(block_table.shape)}")
+    if page_size < 1 or n_rows % page_size != 0:
+        raise GqlaError(f"a cache of {n_rows} rows is not made of pages of {page_size}")
+    return n_rows // page_size
+
+
+def gqla_append_rope(dims: GqlaDims, c: torch.Tensor, k_r: torch.Tensor, new_start: torch.Tensor, seqlens: torch.Tensor,
+                     rope: torch.Tensor, style: str, cache: torch.Tensor, seq_start: torch.Tensor | None,
+                     block_table: torch.Tensor | None = None, page_size: int = 0, q_r: torch.Tensor | None = None,
+                     q_out: torch.Tensor | None = None, status_word: torch.Tensor | None = None) -> None:
+    """Writes the new rows [c ; rotated k_r] to the latent cache [N, r_kv+d_r] (packed: seq_start; paged: block_table and
+    page_size) and rotates their queries q_r [n, h_q, d_r] into q_out.  c [n, r_kv], k_r [n, d_r]: packed over the
+    sequences, sequence b's rows are new_start[b]..new_start[b+1] (int32 [B+1]) and end at position seqlens[b] - 1.
+    rope fp32 [positions, d_r] = [cosines ; sines]; style "pairs" (2i, 2i+1) or "halves" (i, i + d_r/2)."""
+    _on_current_device(c, k_r, new_start, seqlens, rope, cache, seq_start, block_table, q_r, q_out, status_word)
+    n, dtype = c.shape[0], c.dtype
+    B, head, mid = _append_args(dims, n, dtype, k_r, new_start, seqlens, rope, style, q_r, q_out)
+    c_stride = _rows("c", c, (n, dims.r_kv), dtype)
+    cache_stride = _rows("cache", cache, (cache.shape[0], dims.r_kv + dims.d_r), dtype)
+    if (seq_start is None) == (block_table is None):
+        raise GqlaError("either seq_start (packed) or block_table (paged)")
+    if block_table is not None:
+        _pages(cache.shape[0], block_table, page_size, B)
+    else:
+        _contig(seq_start)
+        _shape("seq_start", seq_start, (B,), torch.int64)
+    _check(lib().gqla_append_rope(ctypes.byref(dims), _dtype_code(c), B, n, *head, _ptr(c), c_stride, *mid, _ptr(cache), cache_stride,
+                                  cache.shape[0], _ptr(seq_start), _ptr(block_table), block_table.shape[1] if block_table is not None else 0,
+                                  page_size, _ptr(status_word), _stream()), "gqla_append_rope")
+
+
+def gqla_append_rope_fp8(dims: GqlaDims, c: torch.Tensor, k_r: torch.Tensor, new_start: torch.Tensor, seqlens: torch.Tensor,
+                         rope: torch.Tensor, style: str, cache8: torch.Tensor, page_scale: torch.Tensor, block_table: torch.Tensor,
+                         page_size: int, q_r: torch.Tensor | None = None, q_out: torch.Tensor | None = None,
+                         status_word: torch.Tensor | None = None) -> None:
+    """gqla_append_rope into E4M3 pages: codes cache8 (uint8 [N, r_kv+d_r]) with page_scale fp32 [N / page_size], powers of two
+    that grow with the largest value of a page (its older rows are coded anew)."""
+    _on_current_device(c, k_r, new_start, seqlens, rope, cache8, page_scale, block_table, q_r, q_out, status_word)
+    n, dtype = c.shape[0], c.dtype
+    B, head, mid = _append_args(dims, n, dtype, k_r, new_start, seqlens, rope, style, q_r, q_out)
+    c_stride = _rows("c", c, (n, dims.r_kv), dtype)
+    cache_stride = _rows("cache8", cache8, (cache8.shape[0], dims.r_kv + dims.d_r), torch.uint8)
+    _contig(page_scale)
+    _shape("page_scale", page_scale, (_pages(cache8.shape[0], block_table, page_size, B),), torch.float32)
+    _check(lib().gqla_append_rope_fp8(ctypes.byref(dims), _dtype_code(c), B, n, *head, _ptr(c), c_stride, *mid, _ptr(cache8),
+                                      cache_stride, cache8.shape[0], _ptr(page_scale), _ptr(block_table), block_table.shape[1],
+                                      page_size, _ptr(status_word), _stream()), "gqla_append_rope_fp8")
+
+
+def _planes(dims: GqlaDims, k_c8, v8, k_r8, k_scale, v_scale, r_scale, block_table, page_size, B) -> int:
+    """Checks the E4M3 planes and their scales; returns the row stride of k_r8."""
+    n_rows = k_c8.shape[0]
+    n_pages = _pages(n_rows, block_table, page_size, B)
+    _contig(k_c8, v8, k_scale, v_scale, r_scale)
+    for name, t in (("k_c8", k_c8), ("v8", v8)):
+        _shape(name, t, (n_rows, dims.g, dims.d_h), torch.uint8)
+    for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+        _shape(name, t, (n_pages, dims.g), torch.float32)
+    _shape("r_scale", r_scale, (n_pages,), torch.float32)
+    return _rows("k_r8", k_r8, (n_rows, dims.d_r), torch.uint8)
+
+
+def gqla_append_planes_fp8(dims: GqlaDims, k_c: torch.Tensor, v: torch.Tensor, k_r: torch.Tensor, new_start: torch.Tensor,
+                           seqlens: torch.Tensor, rope: torch.Tensor, style: str, k_c8: torch.Tensor, v8: torch.Tensor,
+                           k_r8: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, r_scale: torch.Tensor,
+                           block_table: torch.Tensor, page_size: int, q_r: torch.Tensor | None = None,
+                           q_out: torch.Tensor | None = None, status_word: torch.Tensor | None = None) -> None:
+    """The GQA path's new rows, k_c, v [n, g, d_h] and k_r [n, d_r] (rotated on the way), into E4M3 planes k_c8, v8 [N, g, d_h],
+    k_r8 [N, d_r] with a scale per page and group (k_scale, v_scale [N / page_size, g]; r_scale [N / page_size])."""
+    _on_current_device(k_c, v, k_r, new_start, seqlens, rope, k_c8, v8, k_r8, k_scale, v_scale, r_scale, block_table, q_r, q_out,
+                       status_word)
+    n, dtype = k_c.shape[0], k_c.dtype
+    B, head, mid = _append_args(dims, n, dtype, k_r, new_start, seqlens, rope, style, q_r, q_out)
+    _contig(k_c, v)
+    for name, t in (("k_c", k_c), ("v", v)):
+        _shape(name, t, (n, dims.g, dims.d_h), dtype)
+    k_r8_stride = _planes(dims, k_c8, v8, k_r8, k_scale, v_scale, r_scale, block_table, page_size, B)
+    _check(lib().gqla_append_planes_fp8(ctypes.byref(dims), _dtype_code(k_c), B, n, *head, _ptr(k_c), _ptr(v), *mid, _ptr(k_c8),
+                                        _ptr(v8), _ptr(k_r8), k_r8_stride, k_c8.shape[0], _ptr(k_scale), _ptr(v_scale),
+                                        _ptr(r_scale), _ptr(block_table), block_table.shape[1], page_size, _ptr(status_word),
+                                        _stream()), "gqla_append_planes_fp8")
+
+
+def _partials(dims: GqlaDims, B: int, s_q: int, num_splits: int, width: int, dtype: torch.dtype, o_part, lse_part, out, lse) -> None:
+    _contig(o_part, lse_part, out, lse)
+    _shape("o_part", o_part, (B, abs(num_splits), s_q, dims.h_q, width), torch.float32)
+    _shape("lse_part", lse_part, (B, abs(num_splits), s_q, dims.h_q), torch.float32)
+    if out is not None:
+        _shape("out", out, (B, s_q, dims.h_q, width), dtype)
+    if lse is not None:
+        _shape("lse", lse, (B, s_q, dims.h_q), torch.float32)
+
+
+def gqla_decode_absorb_fp8_paged(dims: GqlaDims, q_hat: torch.Tensor, cache8: torch.Tensor, page_scale: torch.Tensor,
+                                 block_table: torch.Tensor, page_size: int, seqlens: torch.Tensor, scale: float, num_splits: int,
+                                 o_part: torch.Tensor, lse_part: torch.Tensor, out: torch.Tensor | None = None,
+                                 lse: torch.Tensor | None = None, status_word: torch.Tensor | None = None) -> None:
+    """Absorb-path attention (Eq. (mqa), lines 3-5) over E4M3 pages with a scale per page; q_hat [B,s_q,h_q,r_kv+d_r] in bf16 or
+    fp32.  With `out` [B,s_q,h_q,r_kv] the partials are merged by the same call (lse [B,s_q,h_q] optional)."""
+    _on_current_device(q_hat, cache8, page_scale, block_table, seqlens, o_part, lse_part, out, lse, status_word)
+    B, s_q = q_hat.shape[0], q_hat.shape[1]
+    _contig(q_hat, page_scale, seqlens)
+    _shape("q_hat", q_hat, (B, s_q, dims.h_q, dims.r_kv + dims.d_r), q_hat.dtype)
+    _shape("seqlens", seqlens, (B,), torch.int32)
+    cache_stride = _rows("cache8", cache8, (cache8.shape[0], dims.r_kv + dims.d_r), torch.uint8)
+    _shape("page_scale", page_scale, (_pages(cache8.shape[0], block_table, page_size, B),), torch.float32)
+    _partials(dims, B, s_q, num_splits, dims.r_kv, q_hat.dtype, o_part, lse_part, out, lse)
+    _check(lib().gqla_decode_absorb_fp8_paged(ctypes.byref(dims), _dtype_code(q_hat), B, s_q, scale, num_splits, _ptr(q_hat),
+                                              _ptr(cache8), cache_stride, cache8.shape[0], _ptr(page_scale), _ptr(block_table),
+                                              block_table.shape[1], page_size, _ptr(seqlens), _ptr(o_part), _ptr(lse_part), _ptr(out),
+                                              _ptr(lse), _ptr(status_word), _stream()), "gqla_decode_absorb_fp8_paged")
+
+
+def gqla_decode_gqa_fp8_paged(dims: GqlaDims, q: torch.Tensor, k_c8: torch.Tensor, v8: torch.Tensor, k_r8: torch.Tensor,
+                              k_scale: torch.Tensor, v_scale: torch.Tensor, r_scale: torch.Tensor, block_table: torch.Tensor,
+                              page_size: int, seqlens: torch.Tensor, scale: float, num_splits: int, o_part: torch.Tensor,
+                              lse_part: torch.Tensor, out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+                              status_word: torch.Tensor | None = None) -> None:
+    """GQA-path attention (Eq. (mha)) over E4M3 planes with a scale per page and group; q [B,s_q,h_q,d_h+d_r] in bf16 or fp32.
+    With `out` [B,s_q,h_q,d_h] the partials are merged by the same call (lse [B,s_q,h_q] optional)."""
+    _on_current_device(q, k_c8, v8, k_r8, k_scale, v_scale, r_scale, block_table, seqlens, o_part, lse_part, out, lse, status_word)
+    B, s_q = q.shape[0], q.shape[1]
+    _contig(q, seqlens)
+    _shape("q", q, (B, s_q, dims.h_q, dims.d_h + dims.d_r), q.dtype)
+    _shape("seqlens", seqlens, (B,), torch.int32)
+    k_r8_stride = _planes(dims, k_c8, v8, k_r8, k_scale, v_scale, r_scale, block_table, page_size, B)
+    _partials(dims, B, s_q, num_splits, dims.d_h, q.dtype, o_part, lse_part, out, lse)
+    _check(lib().gqla_decode_gqa_fp8_paged(ctypes.byref(dims), _dtype_code(q), B, s_q, scale, num_splits, _ptr(q), _ptr(k_c8),
+                                           _ptr(v8), _ptr(k_r8), k_r8_stride, k_c8.shape[0], _ptr(k_scale), _ptr(v_scale),
+                                           _ptr(r_scale), _ptr(block_table), block_table.shape[1], page_size, _ptr(seqlens),
+                                           _ptr(o_part), _ptr(lse_part), _ptr(out), _ptr(lse), _ptr(status_word), _stream()),
+           "gqla_decode_gqa_fp8_paged")
+
+
+def gqla_fp8_paged_workers(dims: GqlaDims, dtype: torch.dtype, s_q: int, page_size: int, path: str) -> int:
+    """Workers a balanced call of the two is cut for on the current device (0: fixed plan is used instead)."""
+    code = GQLA_BF16 if dtype == torch.bfloat16 else GQLA_F32
+    return int(lib().gqla_fp8_paged_workers(ctypes.byref(dims), code, s_q, page_size, 0 if path == "absorb" else 1))
 
 
 # ------------------------------------------------------------------ integer helpers (host)

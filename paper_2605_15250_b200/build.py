@@ -8,10 +8,10 @@ import sys
 PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libgqla.so")
-SOURCES = ["gqla_api.cu", "gqla_noalloc.cu"]
+SOURCES = ["gqla_api.cu", "gqla_noalloc.cu", "gqla_fp8_paged.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-    "--expt-relaxed-constexpr", "-shared", "-Xcompiler", "-fPIC", "-cudart", "static",
+    "--expt-relaxed-constexpr", "--threads", "0", "-shared", "-Xcompiler", "-fPIC", "-cudart", "static",
 ]
 
 

@@ -590,4 +590,18 @@ inline bool make_tmap_u8(CUtensorMap* out, const void* base, int rank, const uin
 }
 
 }  // namespace tc
+
+// SMs of the current device (cached per device ordinal); 0 on failure.
+inline int sm_count() {
+    static int cached[64] = {};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+    if (cached[dev] == 0) {
+        int n = 0;
+        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+        cached[dev] = n;
+    }
+    return cached[dev];
+}
+
 }  // namespace gqla

@@ -1,0 +1,584 @@
+// Split-KV flash decoding of both paths over E4M3 pages with a scale per page and head, tokens on the MMA's M axis:
+//
+//   absorb path, Eq. (mqa) lines 3-5    x_t = scale s_t (q_hat . k8_t)                       o = sum_t p_t s_t k8_t[:512] / sum_t p_t
+//   GQA path, Eq. (mha)                 x_t = scale (s^K_t (q_C . kC8_t) + s^R_t (q_R . kR8_t))  o = sum_t p_t s^V_t v8_t / sum_t p_t
+//
+//   S^T = K Q^T     M = 128 tokens, N = R query rows               (A = K tile, B = Q, both K-major)
+//   O^T = V^T P^T   M = 128 value columns, N = 2 R, K = 128 tokens (A = V tile read MN-major, B = P^T rows)
+//
+// Queries and probabilities keep the precision of the bf16 path although the tensor core multiplies E4M3 by E4M3:
+//   * A query row is scaled by a power of two to a maximum in (224, 448] and cut into two codes, q = hi + lo.  Four significant bits
+//     each hold the eight of a bf16 value (the difference from the nearest hi is a multiple of the value's last bit and at most eight
+//     of them), so the scores are those of the bf16 query as long as an element is not below 2^-15 of its row's largest;
+//     what is smaller keeps an absolute error of 2^-19 of the largest.  Both terms' products go into one accumulator.
+//   * With y_t = x_t + log2 s^V_t (log2 units), P'_t = 2^(y_t - m) is the token's weight with its V scale in it, which bounds what
+//     P' has to represent to the token's share of the output.  P' is cut into hi and 16 lo, both E4M3, which multiply into columns
+//     of their own: O = O_hi + O_lo / 16.  Relative error 2^-9 (hi leaves at most 2^-4 of a binade, lo rounds that to four
+//     bits), absolute one 2^-14 where the reference puts the largest P' between 2^6 and 2^8.75: 2^-20 of a row's largest weight.
+//     The sum over p = P' / s^V is taken in fp32 before any rounding.
+// The tensor core does twice the method's products at E4M3 rate, i.e. what the bf16 path pays, on half the bytes.
+//
+//   * The softmax is that of tc_decode_gqa_t.cuh: a TMEM lane is a token, a thread has one token and eight query rows, every thread
+//     holds its rows' references, and the four warps that share rows ask once per tile, in a barrier of their own, whether any score
+//     outgrew its reference by more than kP8Grow binades.  A thread's scales are one page's: its page number is looked up two tiles ahead and its scales one.
+//   * R = 16 or 32 query rows per CTA.  More rows (the absorb path's 128 heads, s_q > 1) are blocks of 32 on CTAs of their own
+//     that walk the same tiles at the same time, so that the cache comes from HBM once and from L2 otherwise.
+//   * Absorb path: V is the latent part of the K tile, which is read in both orders from one place in shared memory.
+//   * Tiles are fetched in boxes of PG rows, the largest of 64, 32 or 16 that divides the page.  What lies behind a sequence's end in its last
+//     page may be anything, NaN codes included: scores are selected by position, V rows are zeros there (CutMaps).
+//   * The softmax warps read the query rows, cut them and write the swizzled operand themselves, at a piece's start.
+//   * Issuer and producer run converged (tc_common.cuh).
+#pragma once
+#include "append_rope.cuh"  // pow2_scale, finite_max
+#include "common.cuh"
+#include "sched.cuh"
+#include "tc_common.cuh"
+#include "tc_decode_gqa_fp8_t.cuh"  // E4M3 descriptors and MMAs, tables in shared memory
+
+namespace gqla {
+namespace tc {
+
+struct Fp8PagedParams {
+    int32_t B, S, s_q, h_q, g, hpg;
+    int32_t hb, hshift;      // heads of a row block (a power of two) and its logarithm: row r is position r >> hshift, head r & (hb - 1)
+    int32_t n_hb, row_blocks;  // row blocks over the heads; over heads and positions
+    int32_t balanced, W;
+    int32_t n_rows, n_pages;
+    float scale_log2;
+    const __nv_bfloat16* q;  // [B, s_q, h_q, 576 or 192]
+    const float *k_scale, *r_scale, *v_scale;  // absorb path: k_scale [pages]; GQA path: [pages, g], [pages], [pages, g]
+    RowMap rows;
+    const int32_t* seqlens;
+    float* o_part;    // [B, S, s_q, h_q, 512 or 128]
+    float* lse_part;  // [B, S, s_q, h_q]
+    int32_t* status;
+};
+
+template <int R, bool LATENT>
+struct Fp8PagedSmem {
+    static constexpr int kBlocks = LATENT ? 4 : 1;           // 128-column blocks of the keys in front of the RoPE part
+    static constexpr int kQTerm = R * (kBlocks * 128 + 64);  // one term of the query rows: blocks of 128 bytes, then 64
+    static constexpr int kQBytes = 2 * kQTerm;
+    static constexpr int kTokBytes = 16384;                  // 128 tokens x 128 bytes
+    static constexpr int kKBytes = kBlocks * kTokBytes + 8192;
+    static constexpr int kVBytes = LATENT ? 0 : kTokBytes;
+    static constexpr int kStageBytes = kKBytes + kVBytes;
+    static constexpr int kStages = LATENT ? 2 : 4;
+    static constexpr int kPRow = 2 * R;                      // one token's hi and lo terms, in runs of eight rows each
+    static constexpr int kPBuf = 128 * kPRow;
+    static constexpr int kOffStage = kQBytes;
+    static constexpr int kOffP = kOffStage + kStages * kStageBytes;
+    static constexpr int kOffRed = kOffP + 2 * kPBuf;        // [4][R] maxima, [R][4] sums; the plan scratch
+    static constexpr int kOffScale = kOffRed + 1024;         // [R] score scales of the piece's query rows
+    static constexpr int kTileBytes = kOffScale + R * 4;
+    // q_full o_free kfull[] vfull[] kempty[] vempty[] s_full[2] p_ready[2] pv_done[2]
+    static constexpr int kNumBars = 2 + 4 * kStages + 6;
+    static constexpr int kSoftmaxWarps = R / 2;              // R / 8 per TMEM lane quadrant
+    static constexpr int kThreads = 64 + 32 * kSoftmaxWarps;
+    static constexpr int kTotal = kTileBytes + kNumBars * 8 + 16;
+    static_assert(R == 16 || R == 32, "");
+    static_assert(kQTerm % 1024 == 0 && kStageBytes % 1024 == 0 && kPBuf % 1024 == 0, "swizzled tiles need 1 KB alignment");
+    static_assert(1024 >= 8 * R * 4 && 1024 >= (3 * 32 + 4) * 4, "");
+    static_assert(kTotal <= 232448, "shared memory budget of one CTA");
+    static_assert(OneCtaPerSM<kTotal>::value, "");
+};
+
+constexpr float kP8Bias = 6.0f;   // log2 units a raised reference sits below the maximum that raised it
+constexpr float kP8Grow = 8.75f;  // a score this far above its reference raises it: 2^8.75 = 430 < 448
+constexpr float kP8Lo = 16.0f;    // scale of the second term
+
+// Two values as two codes each: hi (nearest), lo (nearest to the rest, times kP8Lo).  By way of fp16, whose eleven bits add 2^-12 to the 2^-9.
+__device__ __forceinline__ void split_e4m3x2(float x0, float x1, uint32_t& hi, uint32_t& lo) {
+    asm("{\n\t.reg .b32 h, b, d;\n\t.reg .b16 c, e;\n\t"
+        "cvt.rn.f16x2.f32 h, %3, %2;\n\t"
+        "cvt.rn.satfinite.e4m3x2.f16x2 c, h;\n\t"
+        "cvt.rn.f16x2.e4m3x2 b, c;\n\t"
+        "sub.rn.f16x2 d, h, b;\n\t"
+        "mul.rn.f16x2 d, d, %4;\n\t"
+        "cvt.rn.satfinite.e4m3x2.f16x2 e, d;\n\t"
+        "cvt.u32.u16 %0, c;\n\tcvt.u32.u16 %1, e;\n\t}"
+        : "=r"(hi), "=r"(lo)
+        : "f"(x0), "f"(x1), "r"(0x4c004c00u));  // 16, 16
+}
+
+// OR of a predicate over the `nthreads` threads that call it on named barrier `id`.  (Warps that meet in barriers leave a loop by
+// such a vote, tc_common.cuh.)
+__device__ __forceinline__ bool vote_any(int id, bool v, int nthreads) {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %2, 0;\n\tbarrier.cta.red.or.pred q, %1, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(r)
+        : "r"(id), "r"((uint32_t)v), "r"(nthreads)
+        : "memory");
+    return r != 0;
+}
+
+template <int R, bool LATENT, int PG>
+__global__ void __launch_bounds__(Fp8PagedSmem<R, LATENT>::kThreads, 1)
+decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmR,
+                        const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CutMaps<PG> cut_maps) {
+    using L = Fp8PagedSmem<R, LATENT>;
+    constexpr int NS = L::kStages, NB = 128 / PG;
+    constexpr int KB = L::kBlocks;
+    constexpr int kQWidth = KB * 128 + 64;
+    constexpr int kDv = KB * 128;  // value columns
+    constexpr int kSmT = 32 * L::kSoftmaxWarps;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    uint8_t* tiles = smem_raw;
+    if ((smem_u32(tiles) & 1023u) != 0) {  // swizzled tiles need 1 KB alignment
+        if (threadIdx.x == 0 && p.status != nullptr) atomicCAS(p.status, 0, kStatusTimeout | (15 << 8));
+        return;
+    }
+    uint8_t* q_smem = tiles;
+    uint8_t* stage0 = tiles + L::kOffStage;
+    uint8_t* p_smem = tiles + L::kOffP;
+    float* red = reinterpret_cast<float*>(tiles + L::kOffRed);
+    float* sums = red + 4 * R;
+    float* sm_scale = reinterpret_cast<float*>(tiles + L::kOffScale);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(tiles + L::kTileBytes);
+    uint64_t* q_full = bars + 0;
+    uint64_t* o_free = bars + 1;
+    uint64_t* kfull = bars + 2;
+    uint64_t* vfull = kfull + NS;     // (GQA path)
+    uint64_t* kempty = vfull + NS;
+    uint64_t* vempty = kempty + NS;   // (GQA path)
+    uint64_t* s_full = vempty + NS;   // [2]
+    uint64_t* p_ready = s_full + 2;   // [2]
+    uint64_t* pv_done = p_ready + 2;  // [2]
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + L::kNumBars);
+    volatile int32_t* abort_flag = reinterpret_cast<volatile int32_t*>(tmem_slot + 1);
+
+    // TMEM columns: two score buffers (GQA path: the K_C and the k_R products apart, they have scales of their own), then O^T, one block
+    // of 2 R columns per 128 value columns: row r's hi products in column 16 (r / 8) + r % 8, its lo products eight further on
+    constexpr int kScols = LATENT ? R : 2 * R;
+    constexpr uint32_t kColS = 0, kColO = 2 * kScols, kColsUsed = kColO + KB * 2 * R;
+    constexpr uint32_t kTmemCols = kColsUsed <= 128 ? 128 : (kColsUsed <= 256 ? 256 : 512);
+
+    const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const Abort ab{abort_flag, p.status};
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < L::kNumBars; ++i) {
+            const bool per_warp = &bars[i] == q_full || &bars[i] == o_free || &bars[i] == &p_ready[0] || &bars[i] == &p_ready[1];
+            mbar_init(&bars[i], per_warp ? L::kSoftmaxWarps : 1);
+        }
+        *abort_flag = 0;
+        fence_mbar_init();
+    }
+    if (warp == 1) {
+        tmem_alloc(tmem_slot, kTmemCols);
+        tmem_relinquish();
+    }
+    pdl_launch_dependents();
+    if (warp == 0 && elect_one()) {
+        tma_prefetch_desc(&tmK);
+        tma_prefetch_desc(&tmR);
+        if (!LATENT) tma_prefetch_desc(&tmV);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = warp_uniform(*tmem_slot);
+    pdl_wait();  // set-up is done (behind the preceding kernel's tail); everything below reads the caller's tensors
+    const int rb = blockIdx.x % p.row_blocks;
+    const int j = blockIdx.x / p.row_blocks % p.g;
+    const int unit = blockIdx.x / (p.row_blocks * p.g);
+    const int i0 = rb % p.n_hb * p.hb;                  // first head of this row block in its group
+    const int pq0 = rb / p.n_hb * (R >> p.hshift);      // first query position
+    Walker walk;
+    if (p.balanced) {
+        const BalancedStart st = balanced_prepass(p.seqlens, p.B, p.S, unit, p.W, reinterpret_cast<int32_t*>(red), L::kThreads);
+        walk.init_balanced(p.seqlens, p.B, p.S, unit, p.W, st);
+    } else {
+        walk.init_fixed(p.seqlens, p.B, p.S, unit / p.S, unit % p.S);
+    }
+    Piece pc;
+    int gt = 0;  // tiles walked so far: S / P buffer = gt & 1, phase = (gt >> 1) & 1
+    int pi = 0;  // non-empty pieces walked so far
+
+    if (warp == 0) {
+        // ------------------------------------------------------------------ TMA producer
+        constexpr int kKLoads = NB * (KB + 1);
+        int s = 0;
+        uint32_t ph = 1;  // parity that means "slot is free"
+        bool ok = true;
+        while (ok && walk.next(pc)) {
+            if (pc.n_tiles == 0) continue;
+            const int32_t T = p.seqlens[pc.b];
+            const int run = lane % NB;  // the run of the tile whose row this lane looks up
+            int32_t next_row = p.rows.run_row(pc.b, (uint32_t)(pc.tok_begin + run * PG), T, p.n_rows);
+            for (int t = 0; t < pc.n_tiles; ++t) {
+                const int32_t row = next_row;
+                const int32_t left = T - (pc.tok_begin + t * 128);
+                const int cut = cut_run<PG>(left, 128);
+                if (t + 1 < pc.n_tiles)
+                    next_row = p.rows.run_row(pc.b, (uint32_t)(pc.tok_begin + run * PG) + (uint32_t)(t + 1) * 128u, T, p.n_rows);
+                uint8_t* st = stage0 + s * L::kStageBytes;
+                if (!(ok = warp_all(mbar_wait(&kempty[s], ph, ab, 1)))) break;
+                if (lane == 0) mbar_expect_tx(&kfull[s], L::kKBytes);
+                __syncwarp();
+#pragma unroll
+                for (int i0k = 0; i0k < kKLoads; i0k += 32) {
+                    const int i = i0k + lane, rn = i % NB, blk = i / NB;
+                    const int32_t y = __shfl_sync(0xffffffffu, row, rn);
+                    if (i >= kKLoads) continue;
+                    if (blk < KB) {
+                        if (LATENT) {
+                            if (rn != cut) tma_load_2d(st + blk * L::kTokBytes + rn * PG * 128, &tmK, blk * 128, y, &kfull[s]);
+                        } else {
+                            tma_load_3d(st + rn * PG * 128, &tmK, 0, j, y, &kfull[s]);
+                        }
+                    } else {
+                        tma_load_2d(st + KB * L::kTokBytes + rn * PG * 64, &tmR, LATENT ? 512 : 0, y, &kfull[s]);
+                    }
+                }
+                if (LATENT) {
+                    if (cut >= 0) {
+                        uint8_t* dst = st + cut * PG * 128;
+                        load_cut_run<PG, KB>(cut_maps, lane, left % PG, __shfl_sync(0xffffffffu, row, cut), p.n_rows,
+                                             [&](const CUtensorMap* m, int b, int r, int32_t y) {
+                                                 tma_load_2d(dst + b * L::kTokBytes + r * 128, m, b * 128, y, &kfull[s]);
+                                             });
+                    }
+                } else {
+                    if (!(ok = warp_all(mbar_wait(&vempty[s], ph, ab, 2)))) break;
+                    uint8_t* sv = st + L::kKBytes;
+                    if (lane == 0) mbar_expect_tx(&vfull[s], L::kVBytes);
+                    __syncwarp();
+                    if (lane < NB && lane != cut) tma_load_3d(sv + lane * PG * 128, &tmV, 0, j, row, &vfull[s]);
+                    if (cut >= 0)
+                        load_cut_run<PG, 1>(cut_maps, lane, left % PG, __shfl_sync(0xffffffffu, row, cut), p.n_rows,
+                                            [&](const CUtensorMap* m, int, int r, int32_t y) {
+                                                tma_load_3d(sv + cut * PG * 128 + r * 128, m, 0, j, y, &vfull[s]);
+                                            });
+                }
+                if (++s == NS) { s = 0; ph ^= 1; }
+            }
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ MMA issuer
+        const uint32_t e = elect_one();
+        constexpr uint32_t idesc_qk = idesc_e4m3(128, R, 0, 0);      // S^T: A = K tile (K-major), B = Q (K-major)
+        constexpr uint32_t idesc_pv = idesc_e4m3(128, 2 * R, 1, 1);  // O^T: A = V tile read MN-major, B = P^T rows (MN-major)
+        const uint32_t q_lo = desc_lo(desc_kmajor_sw128(smem_u32(q_smem)));
+        const uint32_t qr_lo = desc_lo(desc_kmajor_sw64(smem_u32(q_smem + KB * R * 128)));
+        const uint64_t pd0 = desc_mnmajor_rows(smem_u32(p_smem), L::kPRow);
+        int ks = 0, vs = 0;
+        uint32_t kph = 0, vph = 0;
+        auto issue_qk = [&](int n) -> bool {
+            if (!warp_all(mbar_wait_fast(&kfull[ks], kph, ab, 3))) return false;
+            tc_fence_after();
+            const uint32_t st = smem_u32(stage0 + ks * L::kStageBytes);
+            const uint32_t d = tmem_base + kColS + (uint32_t)(n & 1) * kScols;
+            const uint32_t k_lo = desc_lo(desc_kmajor_sw128(st)), r_lo = desc_lo(desc_kmajor_sw64(st + KB * L::kTokBytes));
+#pragma unroll
+            for (int term = 0; term < 2; ++term)
+#pragma unroll
+                for (int kk = 0; kk < KB * 4; ++kk)  // 32 elements a step
+                    umma_f8_ss_lo(d, k_lo + ((kk / 4 * L::kTokBytes + kk % 4 * 32) >> 4), kDescHiSw128,
+                                  q_lo + ((term * L::kQTerm + kk / 4 * R * 128 + kk % 4 * 32) >> 4), kDescHiSw128, idesc_qk, (term | kk) != 0, e);
+#pragma unroll
+            for (int term = 0; term < 2; ++term)
+#pragma unroll
+                for (int kk = 0; kk < 2; ++kk)
+                    umma_f8_ss_lo(LATENT ? d : d + R, r_lo + ((kk * 32) >> 4), kDescHiSw64, qr_lo + ((term * L::kQTerm + kk * 32) >> 4),
+                                  kDescHiSw64, idesc_qk, LATENT || (term | kk) != 0, e);
+            if (!LATENT) umma_commit(&kempty[ks], e);
+            umma_commit(&s_full[n & 1], e);
+            if (++ks == NS) { ks = 0; kph ^= 1; }
+            return true;
+        };
+        bool ok = true;
+        while (ok && warp_all(walk.next(pc))) {
+            const int n_tiles = warp_uniform(pc.n_tiles);
+            if (n_tiles == 0) continue;
+            if (!(ok = warp_all(mbar_wait(q_full, pi & 1, ab, 4)))) break;
+            tc_fence_after();
+            if (!(ok = issue_qk(gt))) break;
+            for (int t = 0; t < n_tiles && ok; ++t) {
+                const int n = gt + t;
+                if (t + 1 < n_tiles && !(ok = issue_qk(n + 1))) break;
+                if (!(ok = warp_all(mbar_wait_fast(&p_ready[n & 1], (n >> 1) & 1, ab, 5)))) break;
+                if (t == 0 && pi > 0 && !(ok = warp_all(mbar_wait(o_free, (pi - 1) & 1, ab, 14)))) break;
+                if (!LATENT && !(ok = warp_all(mbar_wait_fast(&vfull[vs], vph, ab, 6)))) break;
+                tc_fence_after();
+                const uint64_t vd = desc_mnmajor_sw128(smem_u32(stage0 + vs * L::kStageBytes + (LATENT ? 0 : L::kKBytes)), 16384);
+                const uint32_t p_lo = (uint32_t)pd0 + (((n & 1) * L::kPBuf) >> 4);
+#pragma unroll
+                for (int m = 0; m < KB; ++m)
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk)  // 32 tokens a step
+                        umma_f8_ss_lo(tmem_base + kColO + (uint32_t)m * 2 * R, (uint32_t)vd + ((m * L::kTokBytes + kk * 4096) >> 4),
+                                      (uint32_t)(vd >> 32), p_lo + ((kk * 32 * L::kPRow) >> 4), (uint32_t)(pd0 >> 32), idesc_pv,
+                                      (t | kk) != 0, e);
+                umma_commit(LATENT ? &kempty[vs] : &vempty[vs], e);
+                umma_commit(&pv_done[n & 1], e);
+                if (++vs == NS) { vs = 0; vph ^= 1; }
+            }
+            gt += n_tiles;
+            ++pi;
+        }
+    } else {
+        // ------------------------------------------------------------------ softmax: one TMEM lane = one token per thread
+        const int q = warp & 3;
+        const int sw = warp - 2;
+        const int part = sw >> 2;      // which eight of the query rows
+        const int r0 = part * 8;
+        const int bar = 2 + part;      // barrier of the four warps that have these rows
+        const int tl = q * 32 + lane;  // token within the tile == TMEM lane (and value column in the output)
+        const uint32_t lane_base = tmem_base + ((uint32_t)(q * 32) << 16);
+        const int sq_left = p.s_q - pq0;  // query positions of this block and behind it
+        // rows [0, r_hi) stand for positions of the step (those of heads behind the group's are computed and dropped)
+        const int r_hi = sq_left < (R >> p.hshift) ? sq_left << p.hshift : R;
+        const int hmask = p.hb - 1;
+        // this thread's sixteen bytes of its token's row of P^T: the hi terms of its eight rows, then the lo terms
+        constexpr uint32_t kPSwz = R == 32 ? 3 : 1;
+        uint8_t* prow = p_smem + tl * L::kPRow + (((uint32_t)part ^ (((uint32_t)(tl * L::kPRow) >> 7) & kPSwz)) << 4);
+        float m_ref[8], l[8];
+
+        auto page_of = [&](uint32_t tok, int32_t T) -> int32_t {  // of a visible token, -1 behind the end
+            return tok < (uint32_t)T ? p.rows.block_table[(int64_t)pc.b * p.rows.max_pages + tok / (uint32_t)p.rows.page_size] : -1;
+        };
+        struct Scales { float k, r, v; };
+        auto scales_of = [&](int32_t page) -> Scales {
+            if ((uint32_t)page >= (uint32_t)p.n_pages) return {1.f, 1.f, 1.f};
+            if (LATENT) {
+                const float s = p.k_scale[page];
+                return {s, s, s};
+            }
+            return {p.k_scale[(int64_t)page * p.g + j], p.r_scale[page], p.v_scale[(int64_t)page * p.g + j]};
+        };
+
+        while (walk.next(pc)) {
+            const int32_t T = p.seqlens[pc.b];
+            const int64_t slot0 = (int64_t)pc.b * p.S;
+            GQLA_DEBUG_CHECK(pc.b >= 0 && pc.b < p.B, p.status, 32);
+            GQLA_DEBUG_CHECK(pc.n_tiles == 0 || (pc.k >= 0 && pc.k < p.S), p.status, 33);
+            GQLA_DEBUG_CHECK(pc.tok_begin >= 0 && pc.tok_begin <= pc.tok_end && pc.tok_end <= (T > 0 ? T : 0), p.status, 34);
+            if (part == 0 && tl < R) {  // split slots this worker marks empty (thread r speaks for row r)
+                const int pq = pq0 + (tl >> p.hshift), il = i0 + (tl & hmask);
+                if (il < p.hpg && pq < p.s_q)
+                    for (int kk = pc.fill_begin; kk < pc.fill_end; ++kk)
+                        p.lse_part[((slot0 + kk) * p.s_q + pq) * p.h_q + (int64_t)j * p.hpg + il] = -INFINITY;
+            }
+            if (pc.n_tiles == 0 && p.balanced) continue;
+            Scales cur{1.f, 1.f, 1.f};
+            int32_t next_page = -1;
+            if (pc.n_tiles > 0) {
+                const uint32_t tok = (uint32_t)(pc.tok_begin + tl);
+                cur = scales_of(page_of(tok, T));
+                next_page = page_of(tok + 128u, T);
+                // ---------------------------------------------------------- the piece's query rows, two a warp
+                // (the scores of the previous piece's last tile have been read, so nothing reads the old rows any more)
+                constexpr int kChunks = kQWidth / 8, kPer = (kChunks + 31) / 32;
+                uint4 u[2][kPer];
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                    const int r = sw + w * L::kSoftmaxWarps, pq = pq0 + (r >> p.hshift), il = i0 + (r & hmask);
+                    const bool valid = il < p.hpg && pq < p.s_q;
+                    const uint4* src = reinterpret_cast<const uint4*>(
+                        p.q + (((int64_t)pc.b * p.s_q + pq) * p.h_q + (int64_t)j * p.hpg + il) * kQWidth);
+#pragma unroll
+                    for (int c = 0; c < kPer; ++c)
+                        u[w][c] = valid && lane + 32 * c < kChunks ? src[lane + 32 * c] : make_uint4(0, 0, 0, 0);
+                }
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                    const int r = sw + w * L::kSoftmaxWarps;
+                    float amax = 0.f;
+#pragma unroll
+                    for (int c = 0; c < kPer; ++c) {
+                        float v[8];
+                        unpack8(u[w][c], v);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) amax = finite_max(amax, v[i]);
+                    }
+                    amax = warp_max(amax);
+                    const float qs = amax > 0.f ? pow2_scale(amax, -110) : 1.f, inv = 1.f / qs;
+#pragma unroll
+                    for (int c = 0; c < kPer; ++c) {
+                        const int ci = lane + 32 * c;
+                        float v[8];
+                        unpack8(u[w][c], v);
+                        uint32_t hi[4], lo[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float x0 = v[2 * i] * inv, x1 = v[2 * i + 1] * inv;
+                            hi[i] = float2_to_e4m3x2(x0, x1);
+                            lo[i] = float2_to_e4m3x2(x0 - e4m3_to_float((uint8_t)(hi[i] & 0xff)), x1 - e4m3_to_float((uint8_t)(hi[i] >> 8)));
+                        }
+                        // blocks of 128 columns: 128-byte rows, 16-byte chunks XORed with r % 8; the RoPE block: 64-byte rows, with r / 2 % 4
+                        const int col = ci * 8, blk = col / 128;
+                        const int off = blk < KB ? blk * R * 128 + r * 128 + ((((col % 128) >> 4) ^ (r & 7)) << 4) + (col & 8)
+                                                 : KB * R * 128 + r * 64 + ((((col - KB * 128) >> 4) ^ ((r >> 1) & 3)) << 4) + (col & 8);
+                        if (ci < kChunks) {
+                            *reinterpret_cast<uint2*>(q_smem + off) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+                            *reinterpret_cast<uint2*>(q_smem + L::kQTerm + off) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+                        }
+                    }
+                    if (lane == 0) sm_scale[r] = p.scale_log2 * qs;
+                }
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(q_full);
+            }
+            named_bar_sync(1, kSmT);  // the scales are there
+#pragma unroll
+            for (int r = 0; r < 8; ++r) { m_ref[r] = kF8NoRef; l[r] = 0.f; }
+            bool ok = true;
+
+            for (int t = 0; t < pc.n_tiles && ok; ++t) {
+                const int n = gt + t;
+                const int s = n & 1;
+                // scales of the next tile and page of the one behind it, on their way while this one is worked on
+                const Scales next = t + 1 < pc.n_tiles ? scales_of(next_page) : Scales{1.f, 1.f, 1.f};
+                if (t + 2 < pc.n_tiles) next_page = page_of((uint32_t)(pc.tok_begin + tl) + (uint32_t)(t + 2) * 128u, T);
+                // (a page without any magnitude has a tiny scale, whose logarithm only has to be finite)
+                const float sv = fmaxf(cur.v, 8.6736174e-19f), lsv = __log2f(sv), inv_sv = __frcp_rn(sv);
+                // A wait that fails raises the CTA's abort flag; the warps agree on leaving at the next barrier below
+                // (a warp that left the loop on its own would strand the others in that barrier).
+                bool okl = __all_sync(0xffffffffu, mbar_wait_fast(&s_full[s], (n >> 1) & 1, ab, 7));
+                // P^T buffer s was last read by P.V(n-2)
+                if (okl && t > 1) okl = __all_sync(0xffffffffu, mbar_wait_fast(&pv_done[s], ((n - 2) >> 1) & 1, ab, 8));
+                tc_fence_after();
+                // rows this thread's token is visible to: the token at absolute position ta is seen by query positions
+                // pq >= s_q - (T - ta); positions behind the step's see nothing
+                const int ta = pc.tok_begin + t * 128 + tl;
+                const int pq_min = sq_left - (T - ta) > 0 ? sq_left - (T - ta) : 0;  // counted from this block's first
+                const int r_lo = ta < pc.tok_end && pq_min < 32 ? (pq_min << p.hshift) : R;
+                float y[8];
+                {
+                    uint32_t x[8], xr[8];
+                    if (okl) {
+                        tmem_ld8(lane_base + kColS + (uint32_t)s * kScols + r0, x);
+                        if (!LATENT) tmem_ld8(lane_base + kColS + (uint32_t)s * kScols + R + r0, xr);
+                        tmem_wait_ld();
+                    }
+                    float rs[8];
+                    load_row<8>(rs, sm_scale + r0);
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        const float dot = LATENT ? __uint_as_float(x[c]) * cur.k
+                                                 : fmaf(__uint_as_float(x[c]), cur.k, __uint_as_float(xr[c]) * cur.r);
+                        y[c] = okl && r0 + c >= r_lo && r0 + c < r_hi ? fmaf(dot, rs[c], lsv) : -INFINITY;
+                    }
+                }
+                bool grow = false;
+#pragma unroll
+                for (int c = 0; c < 8; ++c) grow |= y[c] > m_ref[c] + kP8Grow;
+                if (t == 0 || vote_any(bar, grow || !okl, 128)) {  // a piece's first tile sets the references in any case
+                    float* redw = red + q * R + r0;
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        const float wm = warp_max_redux(y[c]);
+                        if (lane == 0) redw[c] = wm;
+                    }
+                    if (vote_any(bar, !okl, 128)) { ok = false; break; }  // leaving is agreed on (tc_common.cuh)
+                    float factor[8];
+                    bool any = false;
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        const int r = r0 + c;
+                        const float tm = fmaxf(fmaxf(red[r], red[R + r]), fmaxf(red[2 * R + r], red[3 * R + r]));
+                        const bool need = tm > m_ref[c] + kP8Grow;  // (a row that sees nothing yet keeps kF8NoRef)
+                        const float mn = need ? tm - kP8Bias : m_ref[c];
+                        factor[c] = need ? ex2(m_ref[c] - mn) : 1.f;  // ex2(-FLT_MAX - ..) = 0 on first use
+                        any |= need;
+                        l[c] *= factor[c];
+                        m_ref[c] = mn;
+                    }
+                    named_bar_sync(bar, 128);  // red may be rewritten by the next tile
+                    if (any && t > 0) {  // the same in the threads of a warp; no barrier follows inside this branch
+                        // O^T may be rescaled only between P.V(n-1) completing and P.V(n) being issued
+                        if (!__all_sync(0xffffffffu, mbar_wait(&pv_done[(n - 1) & 1], ((n - 1) >> 1) & 1, ab, 8))) {
+                            okl = false;  // noticed by everybody at the next barrier
+                        } else {
+                            tc_fence_after();
+#pragma unroll
+                            for (int m = 0; m < KB; ++m) {
+                                uint32_t o[16];
+                                tmem_ld16(lane_base + kColO + (uint32_t)m * 2 * R + 2 * r0, o);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * factor[c & 7]);
+                                tmem_st16(lane_base + kColO + (uint32_t)m * 2 * R + 2 * r0, o);
+                            }
+                            tmem_wait_st();
+                        }
+                    }
+                }
+                // weights of this token -> its sixteen bytes of P^T
+                uint32_t hi[4], lo[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const float e0 = ex2(y[2 * c] - m_ref[2 * c]), e1 = ex2(y[2 * c + 1] - m_ref[2 * c + 1]);
+                    l[2 * c] = fmaf(e0, inv_sv, l[2 * c]);
+                    l[2 * c + 1] = fmaf(e1, inv_sv, l[2 * c + 1]);
+                    split_e4m3x2(e0, e1, hi[c], lo[c]);
+                }
+                *reinterpret_cast<uint4*>(prow + s * L::kPBuf) =
+                    make_uint4(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16, lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+                fence_proxy_async_smem();  // generic-proxy writes of P^T -> visible to the tensor core
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0 && okl) mbar_arrive(&p_ready[s]);
+                cur = next;
+            }
+
+            // -------------------------------------------------------------- row sums across the 128 tokens, then the output
+            // (the sums do not need the last P.V, so they are exchanged while it runs)
+            warp_sums_scatter<8>(l, lane);
+            if (lane % 4 == 0) sums[4 * (r0 + lane / 4) + q] = l[0];
+            const int n_last = gt + pc.n_tiles - 1;
+            if (pc.n_tiles > 0 && ok)
+                ok = __all_sync(0xffffffffu, mbar_wait_fast(&pv_done[n_last & 1], (n_last >> 1) & 1, ab, 9));
+            tc_fence_after();
+            named_bar_sync(1, kSmT);
+            const int64_t out_row0 = ((slot0 + pc.k) * p.s_q) * p.h_q + (int64_t)j * p.hpg;
+            // lane c finishes row c of the eight, the others get its factor
+            const int rl = lane & 7, r = r0 + rl;
+            float mr = m_ref[0];
+#pragma unroll
+            for (int c = 1; c < 8; ++c) mr = rl == c ? m_ref[c] : mr;
+            const float4 part4 = *reinterpret_cast<const float4*>(sums + 4 * r);
+            const float Lt = (part4.x + part4.y) + (part4.z + part4.w);
+            const bool live = ok && pc.n_tiles > 0 && Lt > 0.f;
+            const float inv = live ? 1.f / Lt : 0.f;
+            {
+                const int pq = pq0 + (r >> p.hshift), il = i0 + (r & hmask);
+                if (q == 0 && lane < 8 && il < p.hpg && pq < p.s_q)
+                    p.lse_part[out_row0 + (int64_t)pq * p.h_q + il] = live ? (mr + log2f(Lt)) * 0.6931471805599453f : -INFINITY;
+            }
+#pragma unroll 1
+            for (int m = 0; m < KB; ++m) {
+                uint32_t o[16];
+                if (pc.n_tiles > 0 && ok) {  // warp-uniform
+                    tmem_ld16(lane_base + kColO + (uint32_t)m * 2 * R + 2 * r0, o);
+                    tmem_wait_ld();
+                }
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    const int rc = r0 + c, pq = pq0 + (rc >> p.hshift), il = i0 + (rc & hmask);
+                    const float f = __shfl_sync(0xffffffffu, inv, c);
+                    // lane tl holds value column 128 m + tl of every row: 128 consecutive floats per row
+                    if (il < p.hpg && pq < p.s_q)
+                        p.o_part[(out_row0 + (int64_t)pq * p.h_q + il) * kDv + m * 128 + tl] =
+                            f > 0.f ? fmaf(__uint_as_float(o[c + 8]), 1.f / kP8Lo, __uint_as_float(o[c])) * f : 0.f;
+                }
+            }
+            named_bar_sync(1, kSmT);  // the tables may be rewritten by the next piece
+            // O^T has been read: the next piece's first P.V may overwrite it
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(o_free);
+            gt += pc.n_tiles;
+            if (pc.n_tiles > 0) ++pi;
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) tmem_dealloc(tmem_base, kTmemCols);
+}
+
+}  // namespace tc
+}  // namespace gqla

@@ -76,19 +76,6 @@ inline bool tc_covers(const gqla_dims& d, gqla_dtype dtype, int32_t s_q, int32_t
     return d.r_kv == 512 && d.d_r == 64 && s_q >= 1 && s_q <= 8;
 }
 
-// SMs of the current device (cached per device ordinal); 0 on failure.
-inline int sm_count() {
-    static int cached[64] = {};
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
-    if (cached[dev] == 0) {
-        int n = 0;
-        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
-        cached[dev] = n;
-    }
-    return cached[dev];
-}
-
 inline int absorb_resident_pairs();
 
 // Query rows of the absorb path's tokens-on-M kernel (tc_decode_absorb_t.cuh): h_q * s_q padded to 16, 32 or 64.
