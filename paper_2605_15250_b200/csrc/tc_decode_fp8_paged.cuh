@@ -57,8 +57,13 @@ struct Fp8PagedParams {
 template <int R, bool LATENT>
 struct Fp8PagedSmem {
     static constexpr int kBlocks = LATENT ? 4 : 1;           // 128-column blocks of the keys in front of the RoPE part
-    static constexpr int kQTerm = R * (kBlocks * 128 + 64);  // one term of the query rows: blocks of 128 bytes, then 64
-    static constexpr int kQBytes = 2 * kQTerm;
+    // Query rows: per 128-column block, and behind these for the RoPE part, 2 R rows of 128 (64) bytes, both terms' -- row r's hi term
+    // in row qrow(r, 0), its lo term in qrow(r, 1).  Absorb path: runs of eight, hi and lo in turn, that multiply into 2 R
+    // columns at once; GQA path: one term behind the other, multiplied into the same R columns.
+    static constexpr bool kTermsApart = LATENT;
+    __device__ static int qrow(int r, int term) { return kTermsApart ? (r >> 3) * 16 + term * 8 + (r & 7) : term * R + r; }
+    static constexpr int kQBlock = 2 * R * 128;
+    static constexpr int kQBytes = kBlocks * kQBlock + 2 * R * 64;
     static constexpr int kTokBytes = 16384;                  // 128 tokens x 128 bytes
     static constexpr int kKBytes = kBlocks * kTokBytes + 8192;
     static constexpr int kVBytes = LATENT ? 0 : kTokBytes;
@@ -77,7 +82,7 @@ struct Fp8PagedSmem {
     static constexpr int kThreads = 64 + 32 * kSoftmaxWarps;
     static constexpr int kTotal = kTileBytes + kNumBars * 8 + 16;
     static_assert(R == 16 || R == 32, "");
-    static_assert(kQTerm % 1024 == 0 && kStageBytes % 1024 == 0 && kPBuf % 1024 == 0, "swizzled tiles need 1 KB alignment");
+    static_assert(kQBytes % 1024 == 0 && kStageBytes % 1024 == 0 && kPBuf % 1024 == 0, "swizzled tiles need 1 KB alignment");
     static_assert(1024 >= 8 * R * 4 && 1024 >= (3 * 32 + 4) * 4, "");
     static_assert(kTotal <= 232448, "shared memory budget of one CTA");
     static_assert(OneCtaPerSM<kTotal>::value, "");
@@ -86,19 +91,37 @@ struct Fp8PagedSmem {
 constexpr float kP8Bias = 6.0f;   // log2 units a raised reference sits below the maximum that raised it
 constexpr float kP8Grow = 8.75f;  // a score this far above its reference raises it: 2^8.75 = 430 < 448
 constexpr float kP8Lo = 16.0f;    // scale of the second term
+constexpr uint32_t kPollSpins = 1u << 25;  // polls (some 40 ns each) after which the issuer gives up
 
-// Two values as two codes each: hi (nearest), lo (nearest to the rest, times kP8Lo).  By way of fp16, whose eleven bits add 2^-12 to the 2^-9.
-__device__ __forceinline__ void split_e4m3x2(float x0, float x1, uint32_t& hi, uint32_t& lo) {
-    asm("{\n\t.reg .b32 h, b, d;\n\t.reg .b16 c, e;\n\t"
+// Two values as two codes each: hi (nearest), lo (nearest to the rest, times kP8Lo).  By way of fp16, whose eleven bits add 2^-12
+// to the 2^-9.
+__device__ __forceinline__ void split_e4m3x2(float x0, float x1, uint16_t& hi, uint16_t& lo) {
+    asm("{\n\t.reg .b32 h, b;\n\t"
         "cvt.rn.f16x2.f32 h, %3, %2;\n\t"
-        "cvt.rn.satfinite.e4m3x2.f16x2 c, h;\n\t"
-        "cvt.rn.f16x2.e4m3x2 b, c;\n\t"
-        "sub.rn.f16x2 d, h, b;\n\t"
-        "mul.rn.f16x2 d, d, %4;\n\t"
-        "cvt.rn.satfinite.e4m3x2.f16x2 e, d;\n\t"
-        "cvt.u32.u16 %0, c;\n\tcvt.u32.u16 %1, e;\n\t}"
-        : "=r"(hi), "=r"(lo)
+        "cvt.rn.satfinite.e4m3x2.f16x2 %0, h;\n\t"
+        "cvt.rn.f16x2.e4m3x2 b, %0;\n\t"
+        "sub.rn.f16x2 b, h, b;\n\t"
+        "mul.rn.f16x2 b, b, %4;\n\t"
+        "cvt.rn.satfinite.e4m3x2.f16x2 %1, b;\n\t}"
+        : "=&h"(hi), "=h"(lo)
         : "f"(x0), "f"(x1), "r"(0x4c004c00u));  // 16, 16
+}
+__device__ __forceinline__ void split_e4m3x4(const float* x, uint32_t& hi, uint32_t& lo) {
+    uint16_t h0, h1, l0, l1;
+    split_e4m3x2(x[0], x[1], h0, l0);
+    split_e4m3x2(x[2], x[3], h1, l1);
+    hi = (uint32_t)h0 | ((uint32_t)h1 << 16);
+    lo = (uint32_t)l0 | ((uint32_t)l1 << 16);
+}
+__device__ __forceinline__ float lg2(float x) {
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float rcp(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
 
 // OR of a predicate over the `nthreads` threads that call it on named barrier `id`.  (Warps that meet in barriers leave a loop by
@@ -148,9 +171,10 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + L::kNumBars);
     volatile int32_t* abort_flag = reinterpret_cast<volatile int32_t*>(tmem_slot + 1);
 
-    // TMEM columns: two score buffers (GQA path: the K_C and the k_R products apart, they have scales of their own), then O^T, one block
-    // of 2 R columns per 128 value columns: row r's hi products in column 16 (r / 8) + r % 8, its lo products eight further on
-    constexpr int kScols = LATENT ? R : 2 * R;
+    // TMEM columns: two score buffers (absorb path: the products with the two terms apart; GQA path: the K_C and the k_R products apart,
+    // they have scales of their own), then O^T, one block of 2 R columns per 128 value columns: row r's hi products in column
+    // 16 (r / 8) + r % 8, its lo products eight further on
+    constexpr int kScols = 2 * R;
     constexpr uint32_t kColS = 0, kColO = 2 * kScols, kColsUsed = kColO + KB * 2 * R;
     constexpr uint32_t kTmemCols = kColsUsed <= 128 ? 128 : (kColsUsed <= 256 ? 256 : 512);
 
@@ -258,62 +282,75 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer
         const uint32_t e = elect_one();
-        constexpr uint32_t idesc_qk = idesc_e4m3(128, R, 0, 0);      // S^T: A = K tile (K-major), B = Q (K-major)
+        constexpr uint32_t idesc_qk = idesc_e4m3(128, L::kTermsApart ? 2 * R : R, 0, 0);  // S^T: A = K tile (K-major), B = Q (K-major)
         constexpr uint32_t idesc_pv = idesc_e4m3(128, 2 * R, 1, 1);  // O^T: A = V tile read MN-major, B = P^T rows (MN-major)
+        constexpr int kTerms = L::kTermsApart ? 1 : 2;               // passes over the keys
         const uint32_t q_lo = desc_lo(desc_kmajor_sw128(smem_u32(q_smem)));
-        const uint32_t qr_lo = desc_lo(desc_kmajor_sw64(smem_u32(q_smem + KB * R * 128)));
+        const uint32_t qr_lo = desc_lo(desc_kmajor_sw64(smem_u32(q_smem + KB * L::kQBlock)));
         const uint64_t pd0 = desc_mnmajor_rows(smem_u32(p_smem), L::kPRow);
         int ks = 0, vs = 0;
         uint32_t kph = 0, vph = 0;
-        auto issue_qk = [&](int n) -> bool {
-            if (!warp_all(mbar_wait_fast(&kfull[ks], kph, ab, 3))) return false;
+        auto issue_qk = [&](int n) {  // the tile is there
             tc_fence_after();
             const uint32_t st = smem_u32(stage0 + ks * L::kStageBytes);
             const uint32_t d = tmem_base + kColS + (uint32_t)(n & 1) * kScols;
             const uint32_t k_lo = desc_lo(desc_kmajor_sw128(st)), r_lo = desc_lo(desc_kmajor_sw64(st + KB * L::kTokBytes));
 #pragma unroll
-            for (int term = 0; term < 2; ++term)
+            for (int term = 0; term < kTerms; ++term)
 #pragma unroll
                 for (int kk = 0; kk < KB * 4; ++kk)  // 32 elements a step
                     umma_f8_ss_lo(d, k_lo + ((kk / 4 * L::kTokBytes + kk % 4 * 32) >> 4), kDescHiSw128,
-                                  q_lo + ((term * L::kQTerm + kk / 4 * R * 128 + kk % 4 * 32) >> 4), kDescHiSw128, idesc_qk, (term | kk) != 0, e);
+                                  q_lo + ((kk / 4 * L::kQBlock + term * R * 128 + kk % 4 * 32) >> 4), kDescHiSw128, idesc_qk, (term | kk) != 0, e);
 #pragma unroll
-            for (int term = 0; term < 2; ++term)
+            for (int term = 0; term < kTerms; ++term)
 #pragma unroll
                 for (int kk = 0; kk < 2; ++kk)
-                    umma_f8_ss_lo(LATENT ? d : d + R, r_lo + ((kk * 32) >> 4), kDescHiSw64, qr_lo + ((term * L::kQTerm + kk * 32) >> 4),
+                    umma_f8_ss_lo(LATENT ? d : d + R, r_lo + ((kk * 32) >> 4), kDescHiSw64, qr_lo + ((term * R * 64 + kk * 32) >> 4),
                                   kDescHiSw64, idesc_qk, LATENT || (term | kk) != 0, e);
             if (!LATENT) umma_commit(&kempty[ks], e);
             umma_commit(&s_full[n & 1], e);
             if (++ks == NS) { ks = 0; kph ^= 1; }
-            return true;
+        };
+        auto issue_pv = [&](int n, bool first) {  // the tile and its weights are there
+            tc_fence_after();
+            const uint64_t vd = desc_mnmajor_sw128(smem_u32(stage0 + vs * L::kStageBytes + (LATENT ? 0 : L::kKBytes)), 16384);
+            const uint32_t p_lo = (uint32_t)pd0 + (((n & 1) * L::kPBuf) >> 4);
+#pragma unroll
+            for (int m = 0; m < KB; ++m)
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk)  // 32 tokens a step
+                    umma_f8_ss_lo(tmem_base + kColO + (uint32_t)m * 2 * R, (uint32_t)vd + ((m * L::kTokBytes + kk * 4096) >> 4),
+                                  (uint32_t)(vd >> 32), p_lo + ((kk * 32 * L::kPRow) >> 4), (uint32_t)(pd0 >> 32), idesc_pv,
+                                  !first || kk != 0, e);
+            umma_commit(LATENT ? &kempty[vs] : &vempty[vs], e);
+            umma_commit(&pv_done[n & 1], e);
+            if (++vs == NS) { vs = 0; vph ^= 1; }
         };
         bool ok = true;
         while (ok && warp_all(walk.next(pc))) {
             const int n_tiles = warp_uniform(pc.n_tiles);
             if (n_tiles == 0) continue;
             if (!(ok = warp_all(mbar_wait(q_full, pi & 1, ab, 4)))) break;
-            tc_fence_after();
-            if (!(ok = issue_qk(gt))) break;
-            for (int t = 0; t < n_tiles && ok; ++t) {
-                const int n = gt + t;
-                if (t + 1 < n_tiles && !(ok = issue_qk(n + 1))) break;
-                if (!(ok = warp_all(mbar_wait_fast(&p_ready[n & 1], (n >> 1) & 1, ab, 5)))) break;
-                if (t == 0 && pi > 0 && !(ok = warp_all(mbar_wait(o_free, (pi - 1) & 1, ab, 14)))) break;
-                if (!LATENT && !(ok = warp_all(mbar_wait_fast(&vfull[vs], vph, ab, 6)))) break;
-                tc_fence_after();
-                const uint64_t vd = desc_mnmajor_sw128(smem_u32(stage0 + vs * L::kStageBytes + (LATENT ? 0 : L::kKBytes)), 16384);
-                const uint32_t p_lo = (uint32_t)pd0 + (((n & 1) * L::kPBuf) >> 4);
-#pragma unroll
-                for (int m = 0; m < KB; ++m)
-#pragma unroll
-                    for (int kk = 0; kk < 4; ++kk)  // 32 tokens a step
-                        umma_f8_ss_lo(tmem_base + kColO + (uint32_t)m * 2 * R, (uint32_t)vd + ((m * L::kTokBytes + kk * 4096) >> 4),
-                                      (uint32_t)(vd >> 32), p_lo + ((kk * 32 * L::kPRow) >> 4), (uint32_t)(pd0 >> 32), idesc_pv,
-                                      (t | kk) != 0, e);
-                umma_commit(LATENT ? &kempty[vs] : &vempty[vs], e);
-                umma_commit(&pv_done[n & 1], e);
-                if (++vs == NS) { vs = 0; vph ^= 1; }
+            // Q K^T goes one tile ahead of P V where the tile is there; a tile that is still on its way does not hold P V up (the
+            // absorb path's slots are only freed by P V)
+            int nq = gt, np = gt;  // next tile of either
+            const int end = gt + n_tiles;
+            uint32_t idle = 0;
+            while (np < end) {
+                if (nq < end && nq - np < 2 && warp_all(mbar_test_wait(&kfull[ks], kph))) {
+                    issue_qk(nq++);
+                    idle = 0;
+                } else if (nq > np && warp_all(mbar_test_wait(&p_ready[np & 1], (np >> 1) & 1))) {
+                    if (np == gt && pi > 0 && !(ok = warp_all(mbar_wait(o_free, (pi - 1) & 1, ab, 14)))) break;
+                    if (!LATENT && !(ok = warp_all(mbar_wait_fast(&vfull[vs], vph, ab, 6)))) break;
+                    issue_pv(np, np == gt);
+                    ++np;
+                    idle = 0;
+                } else if ((++idle & 63u) == 0 && (idle >= kPollSpins || ab.raised())) {
+                    if (idle >= kPollSpins) ab.raise(5);
+                    ok = false;
+                    break;
+                }
             }
             gt += n_tiles;
             ++pi;
@@ -331,14 +368,12 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
         // rows [0, r_hi) stand for positions of the step (those of heads behind the group's are computed and dropped)
         const int r_hi = sq_left < (R >> p.hshift) ? sq_left << p.hshift : R;
         const int hmask = p.hb - 1;
+        const uint32_t page_step = 128u / (uint32_t)p.rows.page_size, page_rest = 128u % (uint32_t)p.rows.page_size;
         // this thread's sixteen bytes of its token's row of P^T: the hi terms of its eight rows, then the lo terms
         constexpr uint32_t kPSwz = R == 32 ? 3 : 1;
         uint8_t* prow = p_smem + tl * L::kPRow + (((uint32_t)part ^ (((uint32_t)(tl * L::kPRow) >> 7) & kPSwz)) << 4);
         float m_ref[8], l[8];
 
-        auto page_of = [&](uint32_t tok, int32_t T) -> int32_t {  // of a visible token, -1 behind the end
-            return tok < (uint32_t)T ? p.rows.block_table[(int64_t)pc.b * p.rows.max_pages + tok / (uint32_t)p.rows.page_size] : -1;
-        };
         struct Scales { float k, r, v; };
         auto scales_of = [&](int32_t page) -> Scales {
             if ((uint32_t)page >= (uint32_t)p.n_pages) return {1.f, 1.f, 1.f};
@@ -363,11 +398,25 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
             }
             if (pc.n_tiles == 0 && p.balanced) continue;
             Scales cur{1.f, 1.f, 1.f};
+            // this thread's token of the tile that is looked up next: its place in its page, its page's in the block table
+            const int32_t* table = p.rows.block_table + (int64_t)pc.b * p.rows.max_pages;
+            uint32_t tok = (uint32_t)(pc.tok_begin + tl);
+            uint32_t col = tok / (uint32_t)p.rows.page_size, at = tok - col * p.rows.page_size;
+            auto next_page_of = [&]() -> int32_t {  // and one tile on
+                const int32_t page = tok < (uint32_t)T ? table[col] : -1;
+                tok += 128u;
+                col += page_step;
+                at += page_rest;
+                if (at >= (uint32_t)p.rows.page_size) {
+                    at -= p.rows.page_size;
+                    ++col;
+                }
+                return page;
+            };
             int32_t next_page = -1;
             if (pc.n_tiles > 0) {
-                const uint32_t tok = (uint32_t)(pc.tok_begin + tl);
-                cur = scales_of(page_of(tok, T));
-                next_page = page_of(tok + 128u, T);
+                cur = scales_of(next_page_of());
+                next_page = next_page_of();
                 // ---------------------------------------------------------- the piece's query rows, two a warp
                 // (the scores of the previous piece's last tile have been read, so nothing reads the old rows any more)
                 constexpr int kChunks = kQWidth / 8, kPer = (kChunks + 31) / 32;
@@ -409,11 +458,12 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
                         }
                         // blocks of 128 columns: 128-byte rows, 16-byte chunks XORed with r % 8; the RoPE block: 64-byte rows, with r / 2 % 4
                         const int col = ci * 8, blk = col / 128;
-                        const int off = blk < KB ? blk * R * 128 + r * 128 + ((((col % 128) >> 4) ^ (r & 7)) << 4) + (col & 8)
-                                                 : KB * R * 128 + r * 64 + ((((col - KB * 128) >> 4) ^ ((r >> 1) & 3)) << 4) + (col & 8);
+                        const int pitch = blk < KB ? 128 : 64;
+                        uint8_t* at = q_smem + (blk < KB ? blk * L::kQBlock + ((((col % 128) >> 4) ^ (r & 7)) << 4)
+                                                         : KB * L::kQBlock + ((((col - KB * 128) >> 4) ^ ((r >> 1) & 3)) << 4)) + (col & 8);
                         if (ci < kChunks) {
-                            *reinterpret_cast<uint2*>(q_smem + off) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
-                            *reinterpret_cast<uint2*>(q_smem + L::kQTerm + off) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+                            *reinterpret_cast<uint2*>(at + L::qrow(r, 0) * pitch) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+                            *reinterpret_cast<uint2*>(at + L::qrow(r, 1) * pitch) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
                         }
                     }
                     if (lane == 0) sm_scale[r] = p.scale_log2 * qs;
@@ -424,53 +474,64 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
             }
             named_bar_sync(1, kSmT);  // the scales are there
 #pragma unroll
-            for (int r = 0; r < 8; ++r) { m_ref[r] = kF8NoRef; l[r] = 0.f; }
+            for (int r = 0; r < 8; ++r) m_ref[r] = l[r] = 0.f;  // (a row that sees a token of the piece sees one of its first tile)
             bool ok = true;
+            // tokens below this are visible to every row of a block without positions behind the step's
+            const int all_end = r_hi < R ? INT32_MIN : (T - (sq_left - 1) < pc.tok_end ? T - (sq_left - 1) : pc.tok_end);
 
             for (int t = 0; t < pc.n_tiles && ok; ++t) {
                 const int n = gt + t;
                 const int s = n & 1;
                 // scales of the next tile and page of the one behind it, on their way while this one is worked on
                 const Scales next = t + 1 < pc.n_tiles ? scales_of(next_page) : Scales{1.f, 1.f, 1.f};
-                if (t + 2 < pc.n_tiles) next_page = page_of((uint32_t)(pc.tok_begin + tl) + (uint32_t)(t + 2) * 128u, T);
-                // (a page without any magnitude has a tiny scale, whose logarithm only has to be finite)
-                const float sv = fmaxf(cur.v, 8.6736174e-19f), lsv = __log2f(sv), inv_sv = __frcp_rn(sv);
+                if (t + 2 < pc.n_tiles) next_page = next_page_of();
+                // (the logarithm of a scale of zero would not be finite)
+                const float sv = fmaxf(cur.v, 8.6736174e-19f), lsv = lg2(sv), inv_sv = rcp(sv);
                 // A wait that fails raises the CTA's abort flag; the warps agree on leaving at the next barrier below
                 // (a warp that left the loop on its own would strand the others in that barrier).
                 bool okl = __all_sync(0xffffffffu, mbar_wait_fast(&s_full[s], (n >> 1) & 1, ab, 7));
                 // P^T buffer s was last read by P.V(n-2)
                 if (okl && t > 1) okl = __all_sync(0xffffffffu, mbar_wait_fast(&pv_done[s], ((n - 2) >> 1) & 1, ab, 8));
                 tc_fence_after();
-                // rows this thread's token is visible to: the token at absolute position ta is seen by query positions
-                // pq >= s_q - (T - ta); positions behind the step's see nothing
-                const int ta = pc.tok_begin + t * 128 + tl;
-                const int pq_min = sq_left - (T - ta) > 0 ? sq_left - (T - ta) : 0;  // counted from this block's first
-                const int r_lo = ta < pc.tok_end && pq_min < 32 ? (pq_min << p.hshift) : R;
-                float y[8];
+                float d[8];  // scores above their references, log2 units
                 {
-                    uint32_t x[8], xr[8];
+                    uint32_t x[16];  // absorb path: the hi and the lo terms' products of rows r0 .. r0 + 7; GQA path: K_C's and k_R's
                     if (okl) {
-                        tmem_ld8(lane_base + kColS + (uint32_t)s * kScols + r0, x);
-                        if (!LATENT) tmem_ld8(lane_base + kColS + (uint32_t)s * kScols + R + r0, xr);
+                        if (LATENT) {
+                            tmem_ld16(lane_base + kColS + (uint32_t)s * kScols + 2 * r0, x);
+                        } else {
+                            tmem_ld8(lane_base + kColS + (uint32_t)s * kScols + r0, x);
+                            tmem_ld8(lane_base + kColS + (uint32_t)s * kScols + R + r0, x + 8);
+                        }
                         tmem_wait_ld();
                     }
                     float rs[8];
                     load_row<8>(rs, sm_scale + r0);
 #pragma unroll
                     for (int c = 0; c < 8; ++c) {
-                        const float dot = LATENT ? __uint_as_float(x[c]) * cur.k
-                                                 : fmaf(__uint_as_float(x[c]), cur.k, __uint_as_float(xr[c]) * cur.r);
-                        y[c] = okl && r0 + c >= r_lo && r0 + c < r_hi ? fmaf(dot, rs[c], lsv) : -INFINITY;
+                        const float x0 = __uint_as_float(x[c]), x1 = __uint_as_float(x[c + 8]);
+                        const float dot = LATENT ? (x0 + x1) * cur.k : fmaf(x0, cur.k, x1 * cur.r);
+                        d[c] = fmaf(dot, rs[c], lsv - m_ref[c]);
                     }
                 }
-                bool grow = false;
+                if (!okl || pc.tok_begin + (t + 1) * 128 > all_end) {
+                    // rows this thread's token is visible to: the token at absolute position ta is seen by query positions
+                    // pq >= s_q - (T - ta); positions behind the step's see nothing
+                    const int ta = pc.tok_begin + t * 128 + tl;
+                    const int pq_min = sq_left - (T - ta) > 0 ? sq_left - (T - ta) : 0;  // counted from this block's first
+                    const int r_lo = okl && ta < pc.tok_end && pq_min < 32 ? (pq_min << p.hshift) : R;
 #pragma unroll
-                for (int c = 0; c < 8; ++c) grow |= y[c] > m_ref[c] + kP8Grow;
-                if (t == 0 || vote_any(bar, grow || !okl, 128)) {  // a piece's first tile sets the references in any case
+                    for (int c = 0; c < 8; ++c)
+                        if (r0 + c < r_lo || r0 + c >= r_hi) d[c] = -INFINITY;
+                }
+                float top = d[0];
+#pragma unroll
+                for (int c = 1; c < 8; ++c) top = fmaxf(top, d[c]);
+                if (t == 0 || vote_any(bar, top > kP8Grow || !okl, 128)) {  // a piece's first tile sets the references in any case
                     float* redw = red + q * R + r0;
 #pragma unroll
                     for (int c = 0; c < 8; ++c) {
-                        const float wm = warp_max_redux(y[c]);
+                        const float wm = warp_max_redux(d[c]);
                         if (lane == 0) redw[c] = wm;
                     }
                     if (vote_any(bar, !okl, 128)) { ok = false; break; }  // leaving is agreed on (tc_common.cuh)
@@ -479,13 +540,14 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
 #pragma unroll
                     for (int c = 0; c < 8; ++c) {
                         const int r = r0 + c;
-                        const float tm = fmaxf(fmaxf(red[r], red[R + r]), fmaxf(red[2 * R + r], red[3 * R + r]));
-                        const bool need = tm > m_ref[c] + kP8Grow;  // (a row that sees nothing yet keeps kF8NoRef)
-                        const float mn = need ? tm - kP8Bias : m_ref[c];
-                        factor[c] = need ? ex2(m_ref[c] - mn) : 1.f;  // ex2(-FLT_MAX - ..) = 0 on first use
+                        const float up = fmaxf(fmaxf(red[r], red[R + r]), fmaxf(red[2 * R + r], red[3 * R + r]));
+                        const bool need = up > (t == 0 ? -FLT_MAX : kP8Grow);
+                        const float by = need ? up - kP8Bias : 0.f;
+                        factor[c] = ex2(-by);  // (on the first tile there is nothing to scale yet)
                         any |= need;
                         l[c] *= factor[c];
-                        m_ref[c] = mn;
+                        m_ref[c] += by;
+                        d[c] -= by;
                     }
                     named_bar_sync(bar, 128);  // red may be rewritten by the next tile
                     if (any && t > 0) {  // the same in the threads of a warp; no barrier follows inside this branch
@@ -508,16 +570,15 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
                     }
                 }
                 // weights of this token -> its sixteen bytes of P^T
-                uint32_t hi[4], lo[4];
+                uint32_t hi[2], lo[2];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const float e0 = ex2(y[2 * c] - m_ref[2 * c]), e1 = ex2(y[2 * c + 1] - m_ref[2 * c + 1]);
-                    l[2 * c] = fmaf(e0, inv_sv, l[2 * c]);
-                    l[2 * c + 1] = fmaf(e1, inv_sv, l[2 * c + 1]);
-                    split_e4m3x2(e0, e1, hi[c], lo[c]);
+                for (int c = 0; c < 8; ++c) {
+                    d[c] = ex2(d[c]);
+                    l[c] = fmaf(d[c], inv_sv, l[c]);
                 }
-                *reinterpret_cast<uint4*>(prow + s * L::kPBuf) =
-                    make_uint4(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16, lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+                split_e4m3x4(d, hi[0], lo[0]);
+                split_e4m3x4(d + 4, hi[1], lo[1]);
+                *reinterpret_cast<uint4*>(prow + s * L::kPBuf) = make_uint4(hi[0], hi[1], lo[0], lo[1]);
                 fence_proxy_async_smem();  // generic-proxy writes of P^T -> visible to the tensor core
                 tc_fence_before();
                 __syncwarp();
