@@ -20,7 +20,8 @@
 //
 //   * The softmax is that of tc_decode_gqa_t.cuh: a TMEM lane is a token, a thread has one token and eight query rows, every thread
 //     holds its rows' references, and the four warps that share rows ask once per tile, in a barrier of their own, whether any score
-//     outgrew its reference by more than kP8Grow binades.  A thread's scales are one page's: its page number is looked up two tiles ahead and its scales one.
+//     outgrew its reference by more than kP8Grow binades.  The producer looks up the scales along with the rows and leaves them in
+//     shared memory.
 //   * R = 16 or 32 query rows per CTA.  More rows (the absorb path's 128 heads, s_q > 1) are blocks of 32 on CTAs of their own
 //     that walk the same tiles at the same time, so that the cache comes from HBM once and from L2 otherwise.
 //   * Absorb path: V is the latent part of the K tile, which is read in both orders from one place in shared memory.
@@ -75,13 +76,18 @@ struct Fp8PagedSmem {
     static constexpr int kOffP = kOffStage + kStages * kStageBytes;
     static constexpr int kOffRed = kOffP + 2 * kPBuf;        // [4][R] maxima, [R][4] sums; the plan scratch
     static constexpr int kOffScale = kOffRed + 1024;         // [R] score scales of the piece's query rows
-    static constexpr int kTileBytes = kOffScale + R * 4;
+    // Scales of the tiles that the producer is ahead by, per run of a page: {K_C or latent, k_R, log2 V, 1 / V}.  The producer
+    // is at most kStages + 1 tiles ahead of the one whose scores are looked at.
+    static constexpr int kScaleTiles = 8;
+    static constexpr int kOffPageScale = kOffScale + 128;
+    static constexpr int kTileBytes = kOffPageScale + kScaleTiles * 8 * 16;
     // q_full o_free kfull[] vfull[] kempty[] vempty[] s_full[2] p_ready[2] pv_done[2]
     static constexpr int kNumBars = 2 + 4 * kStages + 6;
     static constexpr int kSoftmaxWarps = R / 2;              // R / 8 per TMEM lane quadrant
     static constexpr int kThreads = 64 + 32 * kSoftmaxWarps;
     static constexpr int kTotal = kTileBytes + kNumBars * 8 + 16;
     static_assert(R == 16 || R == 32, "");
+    static_assert(kScaleTiles >= kStages + 2 && R * 4 <= 128, "");
     static_assert(kQBytes % 1024 == 0 && kStageBytes % 1024 == 0 && kPBuf % 1024 == 0, "swizzled tiles need 1 KB alignment");
     static_assert(1024 >= 8 * R * 4 && 1024 >= (3 * 32 + 4) * 4, "");
     static_assert(kTotal <= 232448, "shared memory budget of one CTA");
@@ -91,7 +97,7 @@ struct Fp8PagedSmem {
 constexpr float kP8Bias = 6.0f;   // log2 units a raised reference sits below the maximum that raised it
 constexpr float kP8Grow = 8.75f;  // a score this far above its reference raises it: 2^8.75 = 430 < 448
 constexpr float kP8Lo = 16.0f;    // scale of the second term
-constexpr uint32_t kPollSpins = 1u << 25;  // polls (some 40 ns each) after which the issuer gives up
+constexpr uint32_t kPollSpins = 1u << 24;  // polls (some 100 ns each) after which the issuer gives up
 
 // Two values as two codes each: hi (nearest), lo (nearest to the rest, times kP8Lo).  By way of fp16, whose eleven bits add 2^-12
 // to the 2^-9.
@@ -158,6 +164,7 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
     float* red = reinterpret_cast<float*>(tiles + L::kOffRed);
     float* sums = red + 4 * R;
     float* sm_scale = reinterpret_cast<float*>(tiles + L::kOffScale);
+    float4* page_scales = reinterpret_cast<float4*>(tiles + L::kOffPageScale);  // [tile % kScaleTiles][run]
     uint64_t* bars = reinterpret_cast<uint64_t*>(tiles + L::kTileBytes);
     uint64_t* q_full = bars + 0;
     uint64_t* o_free = bars + 1;
@@ -223,22 +230,58 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
     if (warp == 0) {
         // ------------------------------------------------------------------ TMA producer
         constexpr int kKLoads = NB * (KB + 1);
+        const uint32_t page_step = 128u / (uint32_t)p.rows.page_size, page_rest = 128u % (uint32_t)p.rows.page_size;
         int s = 0;
+        int pt = 0;       // tiles loaded so far
         uint32_t ph = 1;  // parity that means "slot is free"
         bool ok = true;
         while (ok && walk.next(pc)) {
             if (pc.n_tiles == 0) continue;
             const int32_t T = p.seqlens[pc.b];
-            const int run = lane % NB;  // the run of the tile whose row this lane looks up
-            int32_t next_row = p.rows.run_row(pc.b, (uint32_t)(pc.tok_begin + run * PG), T, p.n_rows);
-            for (int t = 0; t < pc.n_tiles; ++t) {
-                const int32_t row = next_row;
+            // This lane's run of the tile that is looked up next: its first token, that one's place in its page, the page's in the
+            // block table.  Page numbers are looked up two tiles ahead, scales one.
+            const int run = lane % NB;
+            const int32_t* table = p.rows.block_table + (int64_t)pc.b * p.rows.max_pages;
+            uint32_t tok = (uint32_t)(pc.tok_begin + run * PG);
+            uint32_t col = tok / (uint32_t)p.rows.page_size, at = tok - col * p.rows.page_size;
+            auto next_run = [&](int32_t& page, uint32_t& in_page) {
+                page = tok < (uint32_t)T ? table[col] : -1;  // (the block table says nothing about pages behind the end)
+                in_page = at;
+                tok += 128u;
+                col += page_step;
+                at += page_rest;
+                if (at >= (uint32_t)p.rows.page_size) {
+                    at -= p.rows.page_size;
+                    ++col;
+                }
+            };
+            struct Scales { float k, r, v; };
+            auto scales_of = [&](int32_t page) -> Scales {
+                if ((uint32_t)page >= (uint32_t)p.n_pages) return {1.f, 1.f, 1.f};
+                if (LATENT) {
+                    const float s = p.k_scale[page];
+                    return {s, s, s};
+                }
+                return {p.k_scale[(int64_t)page * p.g + j], p.r_scale[page], p.v_scale[(int64_t)page * p.g + j]};
+            };
+            int32_t page, page1, page2;
+            uint32_t in_page, in_page1, in_page2;
+            next_run(page, in_page);
+            next_run(page1, in_page1);
+            Scales cur = scales_of(page);
+            for (int t = 0; t < pc.n_tiles; ++t, ++pt) {
+                const int32_t row = page < 0 ? p.n_rows : (int32_t)((int64_t)page * p.rows.page_size + in_page);
                 const int32_t left = T - (pc.tok_begin + t * 128);
                 const int cut = cut_run<PG>(left, 128);
-                if (t + 1 < pc.n_tiles)
-                    next_row = p.rows.run_row(pc.b, (uint32_t)(pc.tok_begin + run * PG) + (uint32_t)(t + 1) * 128u, T, p.n_rows);
+                next_run(page2, in_page2);
+                const Scales next = scales_of(page1);
                 uint8_t* st = stage0 + s * L::kStageBytes;
                 if (!(ok = warp_all(mbar_wait(&kempty[s], ph, ab, 1)))) break;
+                if (lane < NB) {  // (the logarithm of a scale of zero would not be finite)
+                    const float sv = fmaxf(cur.v, 8.6736174e-19f);
+                    page_scales[pt % L::kScaleTiles * 8 + lane] = make_float4(cur.k, cur.r, lg2(sv), rcp(sv));
+                }
+                __syncwarp();  // the scales are published with the tile: whoever sees its scores sees them
                 if (lane == 0) mbar_expect_tx(&kfull[s], L::kKBytes);
                 __syncwarp();
 #pragma unroll
@@ -277,6 +320,9 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
                                             });
                 }
                 if (++s == NS) { s = 0; ph ^= 1; }
+                page = page1; in_page = in_page1;
+                page1 = page2; in_page1 = in_page2;
+                cur = next;
             }
         }
     } else if (warp == 1) {
@@ -346,10 +392,13 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
                     issue_pv(np, np == gt);
                     ++np;
                     idle = 0;
-                } else if ((++idle & 63u) == 0 && (idle >= kPollSpins || ab.raised())) {
-                    if (idle >= kPollSpins) ab.raise(5);
-                    ok = false;
-                    break;
+                } else {
+                    __nanosleep(20);
+                    if ((++idle & 63u) == 0 && (idle >= kPollSpins || ab.raised())) {
+                        if (idle >= kPollSpins) ab.raise(5);
+                        ok = false;
+                        break;
+                    }
                 }
             }
             gt += n_tiles;
@@ -368,21 +417,10 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
         // rows [0, r_hi) stand for positions of the step (those of heads behind the group's are computed and dropped)
         const int r_hi = sq_left < (R >> p.hshift) ? sq_left << p.hshift : R;
         const int hmask = p.hb - 1;
-        const uint32_t page_step = 128u / (uint32_t)p.rows.page_size, page_rest = 128u % (uint32_t)p.rows.page_size;
         // this thread's sixteen bytes of its token's row of P^T: the hi terms of its eight rows, then the lo terms
         constexpr uint32_t kPSwz = R == 32 ? 3 : 1;
         uint8_t* prow = p_smem + tl * L::kPRow + (((uint32_t)part ^ (((uint32_t)(tl * L::kPRow) >> 7) & kPSwz)) << 4);
         float m_ref[8], l[8];
-
-        struct Scales { float k, r, v; };
-        auto scales_of = [&](int32_t page) -> Scales {
-            if ((uint32_t)page >= (uint32_t)p.n_pages) return {1.f, 1.f, 1.f};
-            if (LATENT) {
-                const float s = p.k_scale[page];
-                return {s, s, s};
-            }
-            return {p.k_scale[(int64_t)page * p.g + j], p.r_scale[page], p.v_scale[(int64_t)page * p.g + j]};
-        };
 
         while (walk.next(pc)) {
             const int32_t T = p.seqlens[pc.b];
@@ -397,26 +435,7 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
                         p.lse_part[((slot0 + kk) * p.s_q + pq) * p.h_q + (int64_t)j * p.hpg + il] = -INFINITY;
             }
             if (pc.n_tiles == 0 && p.balanced) continue;
-            Scales cur{1.f, 1.f, 1.f};
-            // this thread's token of the tile that is looked up next: its place in its page, its page's in the block table
-            const int32_t* table = p.rows.block_table + (int64_t)pc.b * p.rows.max_pages;
-            uint32_t tok = (uint32_t)(pc.tok_begin + tl);
-            uint32_t col = tok / (uint32_t)p.rows.page_size, at = tok - col * p.rows.page_size;
-            auto next_page_of = [&]() -> int32_t {  // and one tile on
-                const int32_t page = tok < (uint32_t)T ? table[col] : -1;
-                tok += 128u;
-                col += page_step;
-                at += page_rest;
-                if (at >= (uint32_t)p.rows.page_size) {
-                    at -= p.rows.page_size;
-                    ++col;
-                }
-                return page;
-            };
-            int32_t next_page = -1;
             if (pc.n_tiles > 0) {
-                cur = scales_of(next_page_of());
-                next_page = next_page_of();
                 // ---------------------------------------------------------- the piece's query rows, two a warp
                 // (the scores of the previous piece's last tile have been read, so nothing reads the old rows any more)
                 constexpr int kChunks = kQWidth / 8, kPer = (kChunks + 31) / 32;
@@ -482,18 +501,13 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
             for (int t = 0; t < pc.n_tiles && ok; ++t) {
                 const int n = gt + t;
                 const int s = n & 1;
-                // scales of the next tile and page of the one behind it, on their way while this one is worked on
-                const Scales next = t + 1 < pc.n_tiles ? scales_of(next_page) : Scales{1.f, 1.f, 1.f};
-                if (t + 2 < pc.n_tiles) next_page = next_page_of();
-                // (the logarithm of a scale of zero would not be finite)
-                const float sv = fmaxf(cur.v, 8.6736174e-19f), lsv = lg2(sv), inv_sv = rcp(sv);
                 // A wait that fails raises the CTA's abort flag; the warps agree on leaving at the next barrier below
                 // (a warp that left the loop on its own would strand the others in that barrier).
                 bool okl = __all_sync(0xffffffffu, mbar_wait_fast(&s_full[s], (n >> 1) & 1, ab, 7));
                 // P^T buffer s was last read by P.V(n-2)
                 if (okl && t > 1) okl = __all_sync(0xffffffffu, mbar_wait_fast(&pv_done[s], ((n - 2) >> 1) & 1, ab, 8));
                 tc_fence_after();
-                float d[8];  // scores above their references, log2 units
+                float d[8], inv_sv;  // scores above their references, log2 units
                 {
                     uint32_t x[16];  // absorb path: the hi and the lo terms' products of rows r0 .. r0 + 7; GQA path: K_C's and k_R's
                     if (okl) {
@@ -507,12 +521,14 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
                     }
                     float rs[8];
                     load_row<8>(rs, sm_scale + r0);
+                    const float4 ps = page_scales[n % L::kScaleTiles * 8 + tl / PG];
 #pragma unroll
                     for (int c = 0; c < 8; ++c) {
                         const float x0 = __uint_as_float(x[c]), x1 = __uint_as_float(x[c + 8]);
-                        const float dot = LATENT ? (x0 + x1) * cur.k : fmaf(x0, cur.k, x1 * cur.r);
-                        d[c] = fmaf(dot, rs[c], lsv - m_ref[c]);
+                        const float dot = LATENT ? (x0 + x1) * ps.x : fmaf(x0, ps.x, x1 * ps.y);
+                        d[c] = fmaf(dot, rs[c], ps.z - m_ref[c]);
                     }
+                    inv_sv = ps.w;
                 }
                 if (!okl || pc.tok_begin + (t + 1) * 128 > all_end) {
                     // rows this thread's token is visible to: the token at absolute position ta is seen by query positions
@@ -583,7 +599,6 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0 && okl) mbar_arrive(&p_ready[s]);
-                cur = next;
             }
 
             // -------------------------------------------------------------- row sums across the 128 tokens, then the output
