@@ -281,6 +281,8 @@ gqla_status tc_decode_fp8_paged(const Fp8PagedCall& c, cudaStream_t st) {
     p.scale_log2 = c.scale * 1.4426950408889634f;
     p.q = (const __nv_bfloat16*)c.q;
     p.k_scale = c.k_scale; p.r_scale = c.r_scale; p.v_scale = c.v_scale;
+    p.cache = c.k;
+    p.l2_stride = c.latent && c.k_stride <= 640 ? (int32_t)c.k_stride : 0;
     p.rows = RowMap{nullptr, c.block_table, c.max_pages, c.page_size};
     p.seqlens = c.seqlens; p.o_part = c.o_part; p.lse_part = c.lse_part; p.status = c.status;
     cudaError_t e;

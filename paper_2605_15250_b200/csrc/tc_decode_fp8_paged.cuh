@@ -47,6 +47,8 @@ struct Fp8PagedParams {
     int32_t n_rows, n_pages;
     float scale_log2;
     const __nv_bfloat16* q;  // [B, s_q, h_q, 576 or 192]
+    const uint8_t* cache;    // absorb path: the latent rows, for prefetches into L2
+    int32_t l2_stride;       // and the bytes between them; 0: none
     const float *k_scale, *r_scale, *v_scale;  // absorb path: k_scale [pages]; GQA path: [pages, g], [pages], [pages, g]
     RowMap rows;
     const int32_t* seqlens;
@@ -118,6 +120,10 @@ __device__ __forceinline__ void split_e4m3x4(const float* x, uint32_t& hi, uint3
     split_e4m3x2(x[2], x[3], h1, l1);
     hi = (uint32_t)h0 | ((uint32_t)h1 << 16);
     lo = (uint32_t)l0 | ((uint32_t)l1 << 16);
+}
+// Asks for `bytes` (a multiple of 16) to be brought into L2.
+__device__ __forceinline__ void prefetch_l2(const uint8_t* at, uint32_t bytes) {
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(at), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ float lg2(float x) {
     float y;
@@ -229,14 +235,15 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
 
     if (warp == 0) {
         // ------------------------------------------------------------------ TMA producer
-        constexpr int kKLoads = NB * (KB + 1);
+        const uint32_t e = elect_one();
         const uint32_t page_step = 128u / (uint32_t)p.rows.page_size, page_rest = 128u % (uint32_t)p.rows.page_size;
         int s = 0;
         int pt = 0;       // tiles loaded so far
         uint32_t ph = 1;  // parity that means "slot is free"
         bool ok = true;
-        while (ok && walk.next(pc)) {
-            if (pc.n_tiles == 0) continue;
+        while (ok && warp_all(walk.next(pc))) {
+            const int n_tiles = warp_uniform(pc.n_tiles);
+            if (n_tiles == 0) continue;
             const int32_t T = p.seqlens[pc.b];
             // This lane's run of the tile that is looked up next: its first token, that one's place in its page, the page's in the
             // block table.  Page numbers are looked up two tiles ahead, scales one.
@@ -269,12 +276,19 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
             next_run(page, in_page);
             next_run(page1, in_page1);
             Scales cur = scales_of(page);
-            for (int t = 0; t < pc.n_tiles; ++t, ++pt) {
+            for (int t = 0; t < n_tiles; ++t, ++pt) {
                 const int32_t row = page < 0 ? p.n_rows : (int32_t)((int64_t)page * p.rows.page_size + in_page);
                 const int32_t left = T - (pc.tok_begin + t * 128);
-                const int cut = cut_run<PG>(left, 128);
+                const int cut = (int)warp_uniform((uint32_t)cut_run<PG>(left, 128));
                 next_run(page2, in_page2);
                 const Scales next = scales_of(page1);
+                // (a row block each of the tile after next: its rows are in L2 when a slot is free for them)
+                if (LATENT && p.l2_stride > 0 && lane < NB && t + 1 < pc.n_tiles && (t + 1) % p.row_blocks == rb && (uint32_t)page1 < (uint32_t)p.n_pages) {
+                    const int32_t rows_left = left - 128 - run * PG;
+                    const int32_t n = rows_left < PG ? rows_left : PG;
+                    if (n > 0)
+                        prefetch_l2(p.cache + ((int64_t)page1 * p.rows.page_size + in_page1) * p.l2_stride, (uint32_t)((n - 1) * p.l2_stride + 576));
+                }
                 uint8_t* st = stage0 + s * L::kStageBytes;
                 if (!(ok = warp_all(mbar_wait(&kempty[s], ph, ab, 1)))) break;
                 if (lane < NB) {  // (the logarithm of a scale of zero would not be finite)
@@ -282,23 +296,23 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
                     page_scales[pt % L::kScaleTiles * 8 + lane] = make_float4(cur.k, cur.r, lg2(sv), rcp(sv));
                 }
                 __syncwarp();  // the scales are published with the tile: whoever sees its scores sees them
-                if (lane == 0) mbar_expect_tx(&kfull[s], L::kKBytes);
+                mbar_expect_tx(&kfull[s], L::kKBytes, e);
                 __syncwarp();
+                int32_t y[NB];  // first cache row of each run
 #pragma unroll
-                for (int i0k = 0; i0k < kKLoads; i0k += 32) {
-                    const int i = i0k + lane, rn = i % NB, blk = i / NB;
-                    const int32_t y = __shfl_sync(0xffffffffu, row, rn);
-                    if (i >= kKLoads) continue;
-                    if (blk < KB) {
-                        if (LATENT) {
-                            if (rn != cut) tma_load_2d(st + blk * L::kTokBytes + rn * PG * 128, &tmK, blk * 128, y, &kfull[s]);
-                        } else {
-                            tma_load_3d(st + rn * PG * 128, &tmK, 0, j, y, &kfull[s]);
-                        }
-                    } else {
-                        tma_load_2d(st + KB * L::kTokBytes + rn * PG * 64, &tmR, LATENT ? 512 : 0, y, &kfull[s]);
+                for (int rn = 0; rn < NB; ++rn) y[rn] = __shfl_sync(0xffffffffu, row, rn);
+#pragma unroll
+                for (int blk = 0; blk < KB; ++blk)
+#pragma unroll
+                    for (int rn = 0; rn < NB; ++rn) {
+                        if (LATENT)
+                            tma_load_2d(st + blk * L::kTokBytes + rn * PG * 128, &tmK, blk * 128, y[rn], &kfull[s], rn != cut ? e : 0u);
+                        else
+                            tma_load_3d(st + rn * PG * 128, &tmK, 0, j, y[rn], &kfull[s], e);
                     }
-                }
+#pragma unroll
+                for (int rn = 0; rn < NB; ++rn)
+                    tma_load_2d(st + KB * L::kTokBytes + rn * PG * 64, &tmR, LATENT ? 512 : 0, y[rn], &kfull[s], e);
                 if (LATENT) {
                     if (cut >= 0) {
                         uint8_t* dst = st + cut * PG * 128;
@@ -310,9 +324,10 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
                 } else {
                     if (!(ok = warp_all(mbar_wait(&vempty[s], ph, ab, 2)))) break;
                     uint8_t* sv = st + L::kKBytes;
-                    if (lane == 0) mbar_expect_tx(&vfull[s], L::kVBytes);
+                    mbar_expect_tx(&vfull[s], L::kVBytes, e);
                     __syncwarp();
-                    if (lane < NB && lane != cut) tma_load_3d(sv + lane * PG * 128, &tmV, 0, j, row, &vfull[s]);
+#pragma unroll
+                    for (int rn = 0; rn < NB; ++rn) tma_load_3d(sv + rn * PG * 128, &tmV, 0, j, y[rn], &vfull[s], rn != cut ? e : 0u);
                     if (cut >= 0)
                         load_cut_run<PG, 1>(cut_maps, lane, left % PG, __shfl_sync(0xffffffffu, row, cut), p.n_rows,
                                             [&](const CUtensorMap* m, int, int r, int32_t y) {
