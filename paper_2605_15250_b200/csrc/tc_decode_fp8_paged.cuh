@@ -28,7 +28,7 @@
 //   * Tiles are fetched in boxes of PG rows, the largest of 64, 32 or 16 that divides the page.  What lies behind a sequence's end in its last
 //     page may be anything, NaN codes included: scores are selected by position, V rows are zeros there (CutMaps).
 //   * The softmax warps read the query rows, cut them and write the swizzled operand themselves, at a piece's start.
-//   * Issuer and producer run converged (tc_common.cuh).
+//   * Issuers and producer run converged (tc_common.cuh).
 #pragma once
 #include "append_rope.cuh"  // pow2_scale, finite_max
 #include "common.cuh"
@@ -71,27 +71,34 @@ struct Fp8PagedSmem {
     static constexpr int kKBytes = kBlocks * kTokBytes + 8192;
     static constexpr int kVBytes = LATENT ? 0 : kTokBytes;
     static constexpr int kStageBytes = kKBytes + kVBytes;
-    static constexpr int kStages = LATENT ? 2 : 4;
+    static constexpr int kStages = LATENT ? 3 : 4;           // tiles on their way or in use (absorb path: of which some blocks only)
+    // Absorb path: a ring of column blocks (128 tokens x 128 bytes), which P V frees one by one, and one of RoPE blocks, which Q K^T
+    // frees.  Two and a quarter (R = 32) tiles fit; in two stages of a whole tile 64 x 4096 rows took 131 us, 128 heads.
+    static constexpr int kColSlots = LATENT ? (R == 32 ? 9 : 10) : 0;
+    static constexpr int kRingBytes = LATENT ? kColSlots * kTokBytes + kStages * 8192 : kStages * kStageBytes;
     static constexpr int kPRow = 2 * R;                      // one token's hi and lo terms, in runs of eight rows each
     static constexpr int kPBuf = 128 * kPRow;
     static constexpr int kOffStage = kQBytes;
-    static constexpr int kOffP = kOffStage + kStages * kStageBytes;
-    static constexpr int kOffRed = kOffP + 2 * kPBuf;        // [4][R] maxima, [R][4] sums; the plan scratch
-    static constexpr int kOffScale = kOffRed + 1024;         // [R] score scales of the piece's query rows
+    static constexpr int kOffRope = kOffStage + kColSlots * kTokBytes;  // (absorb path)
+    static constexpr int kOffP = kOffStage + kRingBytes;
+    static constexpr int kSoftmaxWarps = R / 2;              // R / 8 per TMEM lane quadrant, eight query rows a thread
+    static constexpr int kOffRed = kOffP + 2 * kPBuf;        // [4][R] maxima, [R][4] sums, [R] factors of a raise, [R] references; the plan scratch
+    static constexpr int kRedBytes = 2048;
+    static constexpr int kOffScale = kOffRed + kRedBytes;    // [R] score scales of the piece's query rows
     // Scales of the tiles that the producer is ahead by, per run of a page: {K_C or latent, k_R, log2 V, 1 / V}.  The producer
     // is at most kStages + 1 tiles ahead of the one whose scores are looked at.
     static constexpr int kScaleTiles = 8;
     static constexpr int kOffPageScale = kOffScale + 128;
     static constexpr int kTileBytes = kOffPageScale + kScaleTiles * 8 * 16;
-    // q_full o_free kfull[] vfull[] kempty[] vempty[] s_full[2] p_ready[2] pv_done[2]
-    static constexpr int kNumBars = 2 + 4 * kStages + 6;
-    static constexpr int kSoftmaxWarps = R / 2;              // R / 8 per TMEM lane quadrant
-    static constexpr int kThreads = 64 + 32 * kSoftmaxWarps;
+    // q_full o_free p_ready[2] pv_done[2] s_full[2] s_empty[2] kfull[] kempty[], GQA path: vfull[] vempty[], absorb path: cempty[]
+    static constexpr int kNumBars = 10 + 2 * kStages + (LATENT ? kColSlots : 2 * kStages);
+    static constexpr int kFirstSoftmax = 4;                  // warps 0, 1, 2: loads, Q K^T, P V
+    static constexpr int kThreads = 32 * (kFirstSoftmax + kSoftmaxWarps);
     static constexpr int kTotal = kTileBytes + kNumBars * 8 + 16;
     static_assert(R == 16 || R == 32, "");
     static_assert(kScaleTiles >= kStages + 2 && R * 4 <= 128, "");
     static_assert(kQBytes % 1024 == 0 && kStageBytes % 1024 == 0 && kPBuf % 1024 == 0, "swizzled tiles need 1 KB alignment");
-    static_assert(1024 >= 8 * R * 4 && 1024 >= (3 * 32 + 4) * 4, "");
+    static_assert(kRedBytes >= 10 * R * 4 && kRedBytes >= (3 * 32 + 4) * 4, "");
     static_assert(kTotal <= 232448, "shared memory budget of one CTA");
     static_assert(OneCtaPerSM<kTotal>::value, "");
 };
@@ -99,7 +106,6 @@ struct Fp8PagedSmem {
 constexpr float kP8Bias = 6.0f;   // log2 units a raised reference sits below the maximum that raised it
 constexpr float kP8Grow = 8.75f;  // a score this far above its reference raises it: 2^8.75 = 430 < 448
 constexpr float kP8Lo = 16.0f;    // scale of the second term
-constexpr uint32_t kPollSpins = 1u << 24;  // polls (some 100 ns each) after which the issuer gives up
 
 // Two values as two codes each: hi (nearest), lo (nearest to the rest, times kP8Lo).  By way of fp16, whose eleven bits add 2^-12
 // to the 2^-9.
@@ -120,6 +126,28 @@ __device__ __forceinline__ void split_e4m3x4(const float* x, uint32_t& hi, uint3
     split_e4m3x2(x[2], x[3], h1, l1);
     hi = (uint32_t)h0 | ((uint32_t)h1 << 16);
     lo = (uint32_t)l0 | ((uint32_t)l1 << 16);
+}
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ uint64_t pack2(float x, float y) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
 }
 // Asks for `bytes` (a multiple of 16) to be brought into L2.
 __device__ __forceinline__ void prefetch_l2(const uint8_t* at, uint32_t bytes) {
@@ -169,22 +197,26 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
     uint8_t* p_smem = tiles + L::kOffP;
     float* red = reinterpret_cast<float*>(tiles + L::kOffRed);
     float* sums = red + 4 * R;
+    float* factors = sums + 4 * R;
+    float* refs = factors + R;
     float* sm_scale = reinterpret_cast<float*>(tiles + L::kOffScale);
     float4* page_scales = reinterpret_cast<float4*>(tiles + L::kOffPageScale);  // [tile % kScaleTiles][run]
     uint64_t* bars = reinterpret_cast<uint64_t*>(tiles + L::kTileBytes);
     uint64_t* q_full = bars + 0;
     uint64_t* o_free = bars + 1;
-    uint64_t* kfull = bars + 2;
-    uint64_t* vfull = kfull + NS;     // (GQA path)
-    uint64_t* kempty = vfull + NS;
-    uint64_t* vempty = kempty + NS;   // (GQA path)
-    uint64_t* s_full = vempty + NS;   // [2]
-    uint64_t* p_ready = s_full + 2;   // [2]
-    uint64_t* pv_done = p_ready + 2;  // [2]
+    uint64_t* p_ready = bars + 2;     // [2]
+    uint64_t* pv_done = bars + 4;     // [2]
+    uint64_t* s_full = bars + 6;      // [2]
+    uint64_t* s_empty = bars + 8;     // [2]
+    uint64_t* kfull = bars + 10;       // the tile's keys (absorb path: all of it)
+    uint64_t* kempty = kfull + NS;    // Q K^T has read them (absorb path: the RoPE part may go)
+    uint64_t* vfull = kempty + NS;    // GQA path
+    uint64_t* vempty = vfull + NS;
+    uint64_t* cempty = kempty + NS;   // absorb path: [kColSlots], P V has read the column block
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + L::kNumBars);
     volatile int32_t* abort_flag = reinterpret_cast<volatile int32_t*>(tmem_slot + 1);
 
-    // TMEM columns: two score buffers (absorb path: the products with the two terms apart; GQA path: the K_C and the k_R products apart,
+    // TMEM columns: the score buffers (absorb path: the products with the two terms apart; GQA path: the K_C and the k_R products apart,
     // they have scales of their own), then O^T, one block of 2 R columns per 128 value columns: row r's hi products in column
     // 16 (r / 8) + r % 8, its lo products eight further on
     constexpr int kScols = 2 * R;
@@ -196,7 +228,7 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < L::kNumBars; ++i) {
-            const bool per_warp = &bars[i] == q_full || &bars[i] == o_free || &bars[i] == &p_ready[0] || &bars[i] == &p_ready[1];
+            const bool per_warp = i < 4 || (&bars[i] >= s_empty && &bars[i] < kfull);  // q_full, o_free, p_ready, s_empty
             mbar_init(&bars[i], per_warp ? L::kSoftmaxWarps : 1);
         }
         *abort_flag = 0;
@@ -237,9 +269,9 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
         // ------------------------------------------------------------------ TMA producer
         const uint32_t e = elect_one();
         const uint32_t page_step = 128u / (uint32_t)p.rows.page_size, page_rest = 128u % (uint32_t)p.rows.page_size;
-        int s = 0;
-        int pt = 0;       // tiles loaded so far
-        uint32_t ph = 1;  // parity that means "slot is free"
+        int s = 0, cs = 0;  // next slots: of tiles, of column blocks
+        int pt = 0;         // tiles loaded so far
+        uint32_t ph = 1, cph = 1;  // parity that means "slot is free"
         bool ok = true;
         while (ok && warp_all(walk.next(pc))) {
             const int n_tiles = warp_uniform(pc.n_tiles);
@@ -252,7 +284,7 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
             uint32_t tok = (uint32_t)(pc.tok_begin + run * PG);
             uint32_t col = tok / (uint32_t)p.rows.page_size, at = tok - col * p.rows.page_size;
             auto next_run = [&](int32_t& page, uint32_t& in_page) {
-                page = tok < (uint32_t)T ? table[col] : -1;  // (the block table says nothing about pages behind the end)
+                page = tok < (uint32_t)T && col < (uint32_t)p.rows.max_pages ? table[col] : -1;  // (the block table says nothing about pages behind the end)
                 in_page = at;
                 tok += 128u;
                 col += page_step;
@@ -289,50 +321,60 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
                     if (n > 0)
                         prefetch_l2(p.cache + ((int64_t)page1 * p.rows.page_size + in_page1) * p.l2_stride, (uint32_t)((n - 1) * p.l2_stride + 576));
                 }
-                uint8_t* st = stage0 + s * L::kStageBytes;
-                if (!(ok = warp_all(mbar_wait(&kempty[s], ph, ab, 1)))) break;
-                if (lane < NB) {  // (the logarithm of a scale of zero would not be finite)
-                    const float sv = fmaxf(cur.v, 8.6736174e-19f);
-                    page_scales[pt % L::kScaleTiles * 8 + lane] = make_float4(cur.k, cur.r, lg2(sv), rcp(sv));
-                }
-                __syncwarp();  // the scales are published with the tile: whoever sees its scores sees them
-                mbar_expect_tx(&kfull[s], L::kKBytes, e);
-                __syncwarp();
                 int32_t y[NB];  // first cache row of each run
 #pragma unroll
                 for (int rn = 0; rn < NB; ++rn) y[rn] = __shfl_sync(0xffffffffu, row, rn);
-#pragma unroll
-                for (int blk = 0; blk < KB; ++blk)
-#pragma unroll
-                    for (int rn = 0; rn < NB; ++rn) {
-                        if (LATENT)
-                            tma_load_2d(st + blk * L::kTokBytes + rn * PG * 128, &tmK, blk * 128, y[rn], &kfull[s], rn != cut ? e : 0u);
-                        else
-                            tma_load_3d(st + rn * PG * 128, &tmK, 0, j, y[rn], &kfull[s], e);
+                const int32_t y_cut = __shfl_sync(0xffffffffu, row, cut < 0 ? 0 : cut);
+                // The tile's scales are published with its first barrier: whoever sees its scores sees them.
+                auto publish_scales = [&]() {
+                    if (lane < NB) {  // (the logarithm of a scale of zero would not be finite)
+                        const float sv = fmaxf(cur.v, 8.6736174e-19f);
+                        page_scales[pt % L::kScaleTiles * 8 + lane] = make_float4(cur.k, cur.r, lg2(sv), rcp(sv));
                     }
+                    __syncwarp();
+                };
+                if constexpr (LATENT) {
+                    if (!(ok = warp_all(mbar_wait(&kempty[s], ph, ab, 1)))) break;
+                    publish_scales();
+                    mbar_expect_tx(&kfull[s], L::kKBytes, e);
+                    __syncwarp();
+                    uint8_t* rope_dst = tiles + L::kOffRope + s * 8192;
 #pragma unroll
-                for (int rn = 0; rn < NB; ++rn)
-                    tma_load_2d(st + KB * L::kTokBytes + rn * PG * 64, &tmR, LATENT ? 512 : 0, y[rn], &kfull[s], e);
-                if (LATENT) {
-                    if (cut >= 0) {
-                        uint8_t* dst = st + cut * PG * 128;
-                        load_cut_run<PG, KB>(cut_maps, lane, left % PG, __shfl_sync(0xffffffffu, row, cut), p.n_rows,
-                                             [&](const CUtensorMap* m, int b, int r, int32_t y) {
-                                                 tma_load_2d(dst + b * L::kTokBytes + r * 128, m, b * 128, y, &kfull[s]);
-                                             });
+                    for (int rn = 0; rn < NB; ++rn) tma_load_2d(rope_dst + rn * PG * 64, &tmR, 512, y[rn], &kfull[s], e);
+#pragma unroll 1
+                    for (int m = 0; m < KB; ++m) {
+                        uint8_t* dst = stage0 + cs * L::kTokBytes;
+                        if (!(ok = warp_all(mbar_wait(&cempty[cs], cph, ab, 2)))) break;
+#pragma unroll
+                        for (int rn = 0; rn < NB; ++rn)
+                            tma_load_2d(dst + rn * PG * 128, &tmK, m * 128, y[rn], &kfull[s], rn != cut ? e : 0u);
+                        if (cut >= 0)
+                            load_cut_run<PG, 1>(cut_maps, lane, left % PG, y_cut, p.n_rows, [&](const CUtensorMap* map, int, int r, int32_t yy) {
+                                tma_load_2d(dst + cut * PG * 128 + r * 128, map, m * 128, yy, &kfull[s]);
+                            });
+                        if (++cs == L::kColSlots) { cs = 0; cph ^= 1; }
                     }
+                    if (!ok) break;
                 } else {
-                    if (!(ok = warp_all(mbar_wait(&vempty[s], ph, ab, 2)))) break;
+                    uint8_t* st = stage0 + s * L::kStageBytes;
                     uint8_t* sv = st + L::kKBytes;
+                    if (!(ok = warp_all(mbar_wait(&kempty[s], ph, ab, 1)))) break;
+                    publish_scales();
+                    mbar_expect_tx(&kfull[s], L::kKBytes, e);
+                    __syncwarp();
+#pragma unroll
+                    for (int rn = 0; rn < NB; ++rn) tma_load_3d(st + rn * PG * 128, &tmK, 0, j, y[rn], &kfull[s], e);
+#pragma unroll
+                    for (int rn = 0; rn < NB; ++rn) tma_load_2d(st + L::kTokBytes + rn * PG * 64, &tmR, 0, y[rn], &kfull[s], e);
+                    if (!(ok = warp_all(mbar_wait(&vempty[s], ph, ab, 2)))) break;
                     mbar_expect_tx(&vfull[s], L::kVBytes, e);
                     __syncwarp();
 #pragma unroll
                     for (int rn = 0; rn < NB; ++rn) tma_load_3d(sv + rn * PG * 128, &tmV, 0, j, y[rn], &vfull[s], rn != cut ? e : 0u);
                     if (cut >= 0)
-                        load_cut_run<PG, 1>(cut_maps, lane, left % PG, __shfl_sync(0xffffffffu, row, cut), p.n_rows,
-                                            [&](const CUtensorMap* m, int, int r, int32_t y) {
-                                                tma_load_3d(sv + cut * PG * 128 + r * 128, m, 0, j, y, &vfull[s]);
-                                            });
+                        load_cut_run<PG, 1>(cut_maps, lane, left % PG, y_cut, p.n_rows, [&](const CUtensorMap* map, int, int r, int32_t yy) {
+                            tma_load_3d(sv + cut * PG * 128 + r * 128, map, 0, j, yy, &vfull[s]);
+                        });
                 }
                 if (++s == NS) { s = 0; ph ^= 1; }
                 page = page1; in_page = in_page1;
@@ -341,100 +383,101 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
             }
         }
     } else if (warp == 1) {
-        // ------------------------------------------------------------------ MMA issuer
+        // ------------------------------------------------------------------ MMA issuer of Q K^T
+        // (Q K^T and P V have a warp each, so that neither waits for what the other needs: absorb path, 64 x 4096 rows, 128 heads 116
+        // us; both in one warp 134)
         const uint32_t e = elect_one();
-        constexpr uint32_t idesc_qk = idesc_e4m3(128, L::kTermsApart ? 2 * R : R, 0, 0);  // S^T: A = K tile (K-major), B = Q (K-major)
-        constexpr uint32_t idesc_pv = idesc_e4m3(128, 2 * R, 1, 1);  // O^T: A = V tile read MN-major, B = P^T rows (MN-major)
-        constexpr int kTerms = L::kTermsApart ? 1 : 2;               // passes over the keys
+        constexpr uint32_t idesc = idesc_e4m3(128, L::kTermsApart ? 2 * R : R, 0, 0);  // S^T: A = K tile (K-major), B = Q (K-major)
+        constexpr int kTerms = L::kTermsApart ? 1 : 2;                                 // passes over the keys
         const uint32_t q_lo = desc_lo(desc_kmajor_sw128(smem_u32(q_smem)));
         const uint32_t qr_lo = desc_lo(desc_kmajor_sw64(smem_u32(q_smem + KB * L::kQBlock)));
-        const uint64_t pd0 = desc_mnmajor_rows(smem_u32(p_smem), L::kPRow);
-        int ks = 0, vs = 0;
-        uint32_t kph = 0, vph = 0;
-        auto issue_qk = [&](int n) {  // the tile is there
-            tc_fence_after();
-            const uint32_t st = smem_u32(stage0 + ks * L::kStageBytes);
-            const uint32_t d = tmem_base + kColS + (uint32_t)(n & 1) * kScols;
-            const uint32_t k_lo = desc_lo(desc_kmajor_sw128(st)), r_lo = desc_lo(desc_kmajor_sw64(st + KB * L::kTokBytes));
-#pragma unroll
-            for (int term = 0; term < kTerms; ++term)
-#pragma unroll
-                for (int kk = 0; kk < KB * 4; ++kk)  // 32 elements a step
-                    umma_f8_ss_lo(d, k_lo + ((kk / 4 * L::kTokBytes + kk % 4 * 32) >> 4), kDescHiSw128,
-                                  q_lo + ((kk / 4 * L::kQBlock + term * R * 128 + kk % 4 * 32) >> 4), kDescHiSw128, idesc_qk, (term | kk) != 0, e);
-#pragma unroll
-            for (int term = 0; term < kTerms; ++term)
-#pragma unroll
-                for (int kk = 0; kk < 2; ++kk)
-                    umma_f8_ss_lo(LATENT ? d : d + R, r_lo + ((kk * 32) >> 4), kDescHiSw64, qr_lo + ((term * R * 64 + kk * 32) >> 4),
-                                  kDescHiSw64, idesc_qk, LATENT || (term | kk) != 0, e);
-            if (!LATENT) umma_commit(&kempty[ks], e);
-            umma_commit(&s_full[n & 1], e);
-            if (++ks == NS) { ks = 0; kph ^= 1; }
-        };
-        auto issue_pv = [&](int n, bool first) {  // the tile and its weights are there
-            tc_fence_after();
-            const uint64_t vd = desc_mnmajor_sw128(smem_u32(stage0 + vs * L::kStageBytes + (LATENT ? 0 : L::kKBytes)), 16384);
-            const uint32_t p_lo = (uint32_t)pd0 + (((n & 1) * L::kPBuf) >> 4);
-#pragma unroll
-            for (int m = 0; m < KB; ++m)
-#pragma unroll
-                for (int kk = 0; kk < 4; ++kk)  // 32 tokens a step
-                    umma_f8_ss_lo(tmem_base + kColO + (uint32_t)m * 2 * R, (uint32_t)vd + ((m * L::kTokBytes + kk * 4096) >> 4),
-                                  (uint32_t)(vd >> 32), p_lo + ((kk * 32 * L::kPRow) >> 4), (uint32_t)(pd0 >> 32), idesc_pv,
-                                  !first || kk != 0, e);
-            umma_commit(LATENT ? &kempty[vs] : &vempty[vs], e);
-            umma_commit(&pv_done[n & 1], e);
-            if (++vs == NS) { vs = 0; vph ^= 1; }
-        };
+        int s = 0, cs = 0;
+        uint32_t ph = 0;
         bool ok = true;
         while (ok && warp_all(walk.next(pc))) {
             const int n_tiles = warp_uniform(pc.n_tiles);
             if (n_tiles == 0) continue;
             if (!(ok = warp_all(mbar_wait(q_full, pi & 1, ab, 4)))) break;
-            // Q K^T goes one tile ahead of P V where the tile is there; a tile that is still on its way does not hold P V up (the
-            // absorb path's slots are only freed by P V)
-            int nq = gt, np = gt;  // next tile of either
-            const int end = gt + n_tiles;
-            uint32_t idle = 0;
-            while (np < end) {
-                if (nq < end && nq - np < 2 && warp_all(mbar_test_wait(&kfull[ks], kph))) {
-                    issue_qk(nq++);
-                    idle = 0;
-                } else if (nq > np && warp_all(mbar_test_wait(&p_ready[np & 1], (np >> 1) & 1))) {
-                    if (np == gt && pi > 0 && !(ok = warp_all(mbar_wait(o_free, (pi - 1) & 1, ab, 14)))) break;
-                    if (!LATENT && !(ok = warp_all(mbar_wait_fast(&vfull[vs], vph, ab, 6)))) break;
-                    issue_pv(np, np == gt);
-                    ++np;
-                    idle = 0;
-                } else {
-                    __nanosleep(20);
-                    if ((++idle & 63u) == 0 && (idle >= kPollSpins || ab.raised())) {
-                        if (idle >= kPollSpins) ab.raise(5);
-                        ok = false;
-                        break;
-                    }
+            for (int t = 0; t < n_tiles; ++t) {
+                const int n = gt + t;
+                if (!(ok = warp_all(mbar_wait_fast(&s_empty[n & 1], ((n >> 1) & 1) ^ 1, ab, 10)))) break;
+                if (!(ok = warp_all(mbar_wait_fast(&kfull[s], ph, ab, 3)))) break;
+                tc_fence_after();
+                const uint32_t d = tmem_base + kColS + (uint32_t)(n & 1) * kScols;
+                const uint8_t* rope = LATENT ? tiles + L::kOffRope + s * 8192 : stage0 + s * L::kStageBytes + L::kTokBytes;
+                const uint32_t r_lo = desc_lo(desc_kmajor_sw64(smem_u32(rope)));
+#pragma unroll
+                for (int m = 0; m < KB; ++m) {
+                    const uint32_t k_lo = desc_lo(desc_kmajor_sw128(smem_u32(stage0 + (LATENT ? cs * L::kTokBytes : s * L::kStageBytes))));
+#pragma unroll
+                    for (int term = 0; term < kTerms; ++term)
+#pragma unroll
+                        for (int kk = 0; kk < 4; ++kk)  // 32 elements a step
+                            umma_f8_ss_lo(d, k_lo + ((kk * 32) >> 4), kDescHiSw128,
+                                          q_lo + ((m * L::kQBlock + term * R * 128 + kk * 32) >> 4), kDescHiSw128, idesc, (m | term | kk) != 0, e);
+                    if (LATENT && ++cs == L::kColSlots) cs = 0;
                 }
+#pragma unroll
+                for (int term = 0; term < kTerms; ++term)
+#pragma unroll
+                    for (int kk = 0; kk < 2; ++kk)
+                        umma_f8_ss_lo(LATENT ? d : d + R, r_lo + ((kk * 32) >> 4), kDescHiSw64, qr_lo + ((term * R * 64 + kk * 32) >> 4),
+                                      kDescHiSw64, idesc, LATENT || (term | kk) != 0, e);
+                umma_commit(&s_full[n & 1], e);
+                umma_commit(&kempty[s], e);
+                if (++s == NS) { s = 0; ph ^= 1; }
             }
             gt += n_tiles;
             ++pi;
         }
-    } else {
+    } else if (warp == 2) {
+        // ------------------------------------------------------------------ MMA issuer of P V
+        const uint32_t e = elect_one();
+        constexpr uint32_t idesc = idesc_e4m3(128, 2 * R, 1, 1);  // O^T: A = V tile read MN-major, B = P^T rows (MN-major)
+        const uint64_t pd0 = desc_mnmajor_rows(smem_u32(p_smem), L::kPRow);
+        int s = 0;  // column block (absorb path) or tile
+        uint32_t ph = 0;
+        bool ok = true;
+        while (ok && warp_all(walk.next(pc))) {
+            const int n_tiles = warp_uniform(pc.n_tiles);
+            if (n_tiles == 0) continue;
+            for (int t = 0; t < n_tiles; ++t) {
+                const int n = gt + t;
+                if (!(ok = warp_all(mbar_wait_fast(&p_ready[n & 1], (n >> 1) & 1, ab, 5)))) break;
+                if (t == 0 && pi > 0 && !(ok = warp_all(mbar_wait(o_free, (pi - 1) & 1, ab, 14)))) break;
+                if (!LATENT && !(ok = warp_all(mbar_wait_fast(&vfull[s], ph, ab, 6)))) break;
+                tc_fence_after();
+                const uint32_t p_lo = (uint32_t)pd0 + (((n & 1) * L::kPBuf) >> 4);
+#pragma unroll
+                for (int m = 0; m < KB; ++m) {
+                    const uint64_t vd = desc_mnmajor_sw128(smem_u32(stage0 + (LATENT ? s * L::kTokBytes : s * L::kStageBytes + L::kKBytes)), 16384);
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk)  // 32 tokens a step
+                        umma_f8_ss_lo(tmem_base + kColO + (uint32_t)m * 2 * R, (uint32_t)vd + ((kk * 4096) >> 4), (uint32_t)(vd >> 32),
+                                      p_lo + ((kk * 32 * L::kPRow) >> 4), (uint32_t)(pd0 >> 32), idesc, (t | kk) != 0, e);
+                    umma_commit(LATENT ? &cempty[s] : &vempty[s], e);
+                    if (++s == (LATENT ? L::kColSlots : NS)) { s = 0; ph ^= 1; }
+                }
+                umma_commit(&pv_done[n & 1], e);
+            }
+            gt += n_tiles;
+            ++pi;
+        }
+    } else if (warp >= L::kFirstSoftmax) {
         // ------------------------------------------------------------------ softmax: one TMEM lane = one token per thread
         const int q = warp & 3;
-        const int sw = warp - 2;
-        const int part = sw >> 2;      // which eight of the query rows
+        const int sw = warp - L::kFirstSoftmax;
+        const int part = sw >> 2;            // which eight of the query rows
         const int r0 = part * 8;
-        const int bar = 2 + part;      // barrier of the four warps that have these rows
-        const int tl = q * 32 + lane;  // token within the tile == TMEM lane (and value column in the output)
+        const int bar = 2 + part;            // barrier of the four warps that have these rows
+        const int tl = q * 32 + lane;        // token within the tile == TMEM lane (and value column in the output)
         const uint32_t lane_base = tmem_base + ((uint32_t)(q * 32) << 16);
         const int sq_left = p.s_q - pq0;  // query positions of this block and behind it
         // rows [0, r_hi) stand for positions of the step (those of heads behind the group's are computed and dropped)
         const int r_hi = sq_left < (R >> p.hshift) ? sq_left << p.hshift : R;
         const int hmask = p.hb - 1;
         // this thread's sixteen bytes of its token's row of P^T: the hi terms of its eight rows, then the lo terms
-        constexpr uint32_t kPSwz = R == 32 ? 3 : 1;
-        uint8_t* prow = p_smem + tl * L::kPRow + (((uint32_t)part ^ (((uint32_t)(tl * L::kPRow) >> 7) & kPSwz)) << 4);
+        uint8_t* prow = p_smem + tl * L::kPRow + (((uint32_t)part ^ (((uint32_t)(tl * L::kPRow) >> 7) & (R == 32 ? 3u : 1u))) << 4);
         float m_ref[8], l[8];
 
         while (walk.next(pc)) {
@@ -519,29 +562,33 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
                 // A wait that fails raises the CTA's abort flag; the warps agree on leaving at the next barrier below
                 // (a warp that left the loop on its own would strand the others in that barrier).
                 bool okl = __all_sync(0xffffffffu, mbar_wait_fast(&s_full[s], (n >> 1) & 1, ab, 7));
-                // P^T buffer s was last read by P.V(n-2)
-                if (okl && t > 1) okl = __all_sync(0xffffffffu, mbar_wait_fast(&pv_done[s], ((n - 2) >> 1) & 1, ab, 8));
                 tc_fence_after();
                 float d[8], inv_sv;  // scores above their references, log2 units
                 {
                     uint32_t x[16];  // absorb path: the hi and the lo terms' products of rows r0 .. r0 + 7; GQA path: K_C's and k_R's
                     if (okl) {
+                        const uint32_t at = lane_base + kColS + (uint32_t)s * kScols;
                         if (LATENT) {
-                            tmem_ld16(lane_base + kColS + (uint32_t)s * kScols + 2 * r0, x);
+                            tmem_ld16(at + 2 * r0, x);
                         } else {
-                            tmem_ld8(lane_base + kColS + (uint32_t)s * kScols + r0, x);
-                            tmem_ld8(lane_base + kColS + (uint32_t)s * kScols + R + r0, x + 8);
+                            tmem_ld8(at + r0, x);
+                            tmem_ld8(at + R + r0, x + 8);
                         }
                         tmem_wait_ld();
                     }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0 && okl) mbar_arrive(&s_empty[s]);  // the scores have been read
                     float rs[8];
                     load_row<8>(rs, sm_scale + r0);
                     const float4 ps = page_scales[n % L::kScaleTiles * 8 + tl / PG];
+                    const uint64_t s0 = pack2(ps.x, ps.x), s1 = pack2(ps.y, ps.y), up = pack2(ps.z, ps.z), minus = pack2(-1.f, -1.f);
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        const float x0 = __uint_as_float(x[c]), x1 = __uint_as_float(x[c + 8]);
-                        const float dot = LATENT ? (x0 + x1) * ps.x : fmaf(x0, ps.x, x1 * ps.y);
-                        d[c] = fmaf(dot, rs[c], ps.z - m_ref[c]);
+                    for (int c = 0; c < 8; c += 2) {
+                        const uint64_t x0 = pack2(__uint_as_float(x[c]), __uint_as_float(x[c + 1]));
+                        const uint64_t x1 = pack2(__uint_as_float(x[c + 8]), __uint_as_float(x[c + 9]));
+                        const uint64_t dot = LATENT ? mul2(add2(x0, x1), s0) : fma2(x0, s0, mul2(x1, s1));
+                        unpack2(fma2(dot, pack2(rs[c], rs[c + 1]), fma2(pack2(m_ref[c], m_ref[c + 1]), minus, up)), d[c], d[c + 1]);
                     }
                     inv_sv = ps.w;
                 }
@@ -566,7 +613,7 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
                         if (lane == 0) redw[c] = wm;
                     }
                     if (vote_any(bar, !okl, 128)) { ok = false; break; }  // leaving is agreed on (tc_common.cuh)
-                    float factor[8];
+                    float* factor = factors + r0;
                     bool any = false;
 #pragma unroll
                     for (int c = 0; c < 8; ++c) {
@@ -574,20 +621,21 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
                         const float up = fmaxf(fmaxf(red[r], red[R + r]), fmaxf(red[2 * R + r], red[3 * R + r]));
                         const bool need = up > (t == 0 ? -FLT_MAX : kP8Grow);
                         const float by = need ? up - kP8Bias : 0.f;
-                        factor[c] = ex2(-by);  // (on the first tile there is nothing to scale yet)
+                        const float f = ex2(-by);  // (on the first tile there is nothing to scale yet)
                         any |= need;
-                        l[c] *= factor[c];
+                        l[c] *= f;
                         m_ref[c] += by;
                         d[c] -= by;
+                        if (lane == 0) factor[c] = f;  // (the same from the four warps)
                     }
-                    named_bar_sync(bar, 128);  // red may be rewritten by the next tile
-                    if (any && t > 0) {  // the same in the threads of a warp; no barrier follows inside this branch
+                    named_bar_sync(bar, 128);  // red may be rewritten by the next tile; the factors are there
+                    if (any && t > 0) {  // the same in the four warps; no barrier follows inside this branch
                         // O^T may be rescaled only between P.V(n-1) completing and P.V(n) being issued
                         if (!__all_sync(0xffffffffu, mbar_wait(&pv_done[(n - 1) & 1], ((n - 1) >> 1) & 1, ab, 8))) {
                             okl = false;  // noticed by everybody at the next barrier
                         } else {
                             tc_fence_after();
-#pragma unroll
+#pragma unroll 1
                             for (int m = 0; m < KB; ++m) {
                                 uint32_t o[16];
                                 tmem_ld16(lane_base + kColO + (uint32_t)m * 2 * R + 2 * r0, o);
@@ -600,12 +648,15 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
                         }
                     }
                 }
+                // P^T buffer s was last read by P.V(n-2)
+                if (okl && t > 1) okl = __all_sync(0xffffffffu, mbar_wait_fast(&pv_done[s], ((n - 2) >> 1) & 1, ab, 8));
                 // weights of this token -> its sixteen bytes of P^T
                 uint32_t hi[2], lo[2];
 #pragma unroll
-                for (int c = 0; c < 8; ++c) {
+                for (int c = 0; c < 8; c += 2) {
                     d[c] = ex2(d[c]);
-                    l[c] = fmaf(d[c], inv_sv, l[c]);
+                    d[c + 1] = ex2(d[c + 1]);
+                    unpack2(fma2(pack2(d[c], d[c + 1]), pack2(inv_sv, inv_sv), pack2(l[c], l[c + 1])), l[c], l[c + 1]);
                 }
                 split_e4m3x4(d, hi[0], lo[0]);
                 split_e4m3x4(d + 4, hi[1], lo[1]);
@@ -620,6 +671,7 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
             // (the sums do not need the last P.V, so they are exchanged while it runs)
             warp_sums_scatter<8>(l, lane);
             if (lane % 4 == 0) sums[4 * (r0 + lane / 4) + q] = l[0];
+            if (q == 0 && lane == 0) store_row<8>(refs + r0, m_ref);
             const int n_last = gt + pc.n_tiles - 1;
             if (pc.n_tiles > 0 && ok)
                 ok = __all_sync(0xffffffffu, mbar_wait_fast(&pv_done[n_last & 1], (n_last >> 1) & 1, ab, 9));
@@ -627,34 +679,36 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
             named_bar_sync(1, kSmT);
             const int64_t out_row0 = ((slot0 + pc.k) * p.s_q) * p.h_q + (int64_t)j * p.hpg;
             // lane c finishes row c of the eight, the others get its factor
-            const int rl = lane & 7, r = r0 + rl;
-            float mr = m_ref[0];
-#pragma unroll
-            for (int c = 1; c < 8; ++c) mr = rl == c ? m_ref[c] : mr;
-            const float4 part4 = *reinterpret_cast<const float4*>(sums + 4 * r);
-            const float Lt = (part4.x + part4.y) + (part4.z + part4.w);
-            const bool live = ok && pc.n_tiles > 0 && Lt > 0.f;
-            const float inv = live ? 1.f / Lt : 0.f;
+            float f;
             {
-                const int pq = pq0 + (r >> p.hshift), il = i0 + (r & hmask);
+                const int r = r0 + lane % 8, pq = pq0 + (r >> p.hshift), il = i0 + (r & hmask);
+                const float4 s4 = *reinterpret_cast<const float4*>(sums + 4 * r);
+                const float Lt = ok && pc.n_tiles > 0 ? (s4.x + s4.y) + (s4.z + s4.w) : 0.f;
+                f = Lt > 0.f ? 1.f / Lt : 0.f;
                 if (q == 0 && lane < 8 && il < p.hpg && pq < p.s_q)
-                    p.lse_part[out_row0 + (int64_t)pq * p.h_q + il] = live ? (mr + log2f(Lt)) * 0.6931471805599453f : -INFINITY;
+                    p.lse_part[out_row0 + (int64_t)pq * p.h_q + il] = Lt > 0.f ? (refs[r] + log2f(Lt)) * 0.6931471805599453f : -INFINITY;
             }
 #pragma unroll 1
             for (int m = 0; m < KB; ++m) {
-                uint32_t o[16];
+                float acc[8];
+#pragma unroll
+                for (int c = 0; c < 8; ++c) acc[c] = 0.f;
                 if (pc.n_tiles > 0 && ok) {  // warp-uniform
-                    tmem_ld16(lane_base + kColO + (uint32_t)m * 2 * R + 2 * r0, o);
+                    uint32_t o[2][8];        // hi and lo terms' products
+                    tmem_ld8(lane_base + kColO + (uint32_t)m * 2 * R + 2 * r0, o[0]);
+                    tmem_ld8(lane_base + kColO + (uint32_t)m * 2 * R + 2 * r0 + 8, o[1]);
                     tmem_wait_ld();
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        const float w = __shfl_sync(0xffffffffu, f, c);
+                        if (w > 0.f) acc[c] = fmaf(__uint_as_float(o[1][c]), 1.f / kP8Lo, __uint_as_float(o[0][c])) * w;
+                    }
                 }
 #pragma unroll
                 for (int c = 0; c < 8; ++c) {
                     const int rc = r0 + c, pq = pq0 + (rc >> p.hshift), il = i0 + (rc & hmask);
-                    const float f = __shfl_sync(0xffffffffu, inv, c);
                     // lane tl holds value column 128 m + tl of every row: 128 consecutive floats per row
-                    if (il < p.hpg && pq < p.s_q)
-                        p.o_part[(out_row0 + (int64_t)pq * p.h_q + il) * kDv + m * 128 + tl] =
-                            f > 0.f ? fmaf(__uint_as_float(o[c + 8]), 1.f / kP8Lo, __uint_as_float(o[c])) * f : 0.f;
+                    if (il < p.hpg && pq < p.s_q) p.o_part[(out_row0 + (int64_t)pq * p.h_q + il) * kDv + m * 128 + tl] = acc[c];
                 }
             }
             named_bar_sync(1, kSmT);  // the tables may be rewritten by the next piece
