@@ -44,6 +44,22 @@ struct NewRows {
     __device__ __forceinline__ int32_t first_pos(int32_t b) const { return seqlens[b] - (start[b + 1] - start[b]); }
 };
 
+// Largest b in [0, B) with at(b) <= x, at ascending, at(0) <= x: a load per lane and round, 32-fold per round (a bisection is a chain of
+// loads, which is what a step's append waits for).  All lanes of the warp call it.
+template <typename F>
+__device__ __forceinline__ int32_t warp_last(int32_t B, int32_t x, F at) {
+    const int lane = threadIdx.x & 31;
+    int32_t lo = 0, size = B;
+    while (size > 1) {
+        const int32_t step = (size + 31) >> 5, i = lane * step;
+        const int32_t c = __popc(__ballot_sync(0xffffffffu, i < size && at(lo + (i < size ? i : 0)) <= x));
+        const int32_t skip = (c > 0 ? c - 1 : 0) * step;
+        lo += skip;
+        size = size - skip < step ? size - skip : step;
+    }
+    return lo;
+}
+
 struct RopeTable {
     const float* cs;  // [rows, d_r]: cosines in the first half of a row, sines in the second
     int32_t rows, d_r, halves;  // halves: pairs (i, i + d_r / 2), otherwise (2 i, 2 i + 1)
@@ -192,54 +208,88 @@ struct AppendArgs {
     void* cache;
     int64_t cache_stride, cache_rows;
     RowMap rows;
-    int32_t per_block, kv_blocks;  // new rows of a block; blocks behind kv_blocks rotate queries
+    int32_t per_warp, kv_blocks;  // new rows of a warp; blocks behind kv_blocks rotate queries
     int32_t* status;
 };
 
-constexpr int kAppendMostRows = 16;
+constexpr int kAppendMostRows = 8;  // new rows of a warp
 
+// Item i, i + step, i + 2 step, .. of rows of `per` items each, without a division per item.
+struct RowItems {
+    int row, col, row_step, col_step, per;
+    __device__ __forceinline__ RowItems(int i, int step, int per_)
+        : row(i / per_), col(i % per_), row_step(step / per_), col_step(step % per_), per(per_) {}
+    __device__ __forceinline__ void next() {
+        row += row_step;
+        col += col_step;
+        if (col >= per) {
+            col -= per;
+            ++row;
+        }
+    }
+};
+
+// A warp takes per_warp new rows: their places are looked up by a lane each, the latent parts copied eight 16-byte vectors a lane
+// at a time (49000 rows of 1152 bytes: 41.7 us with a block per sixteen rows and one vector a thread in flight), the RoPE parts rotated an
+// item a lane.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kAppendThreads) append_rope_kernel(const AppendArgs a) {
-    __shared__ int64_t dst_row[kAppendMostRows];
-    __shared__ int32_t position[kAppendMostRows];
     tc::pdl_launch_dependents();
     tc::pdl_wait();
     if ((int)blockIdx.x >= a.kv_blocks)
         return rotate_queries<T, VEC>(a.nr, a.rope, a.q, (int64_t)(blockIdx.x - a.kv_blocks) * kAppendThreads + threadIdx.x, a.status);
-    const int64_t tok0 = (int64_t)blockIdx.x * a.per_block;
-    const int n = (int)(a.nr.n - tok0 < a.per_block ? a.nr.n - tok0 : a.per_block);
-    if ((int)threadIdx.x < n) {
-        const int32_t tok = (int32_t)tok0 + threadIdx.x, b = a.nr.seq_of(tok);
-        const int32_t pos = a.nr.first_pos(b) + tok - a.nr.start[b];
-        int64_t row = -1;
-        if (pos >= a.rope.rows && a.rope.d_r > 0) append_error(a.status, 1);
-        else if (pos >= 0) row = checked_row(a.rows, b, pos, a.cache_rows, a.status);
-        dst_row[threadIdx.x] = row;
-        position[threadIdx.x] = pos;
-    }
-    __syncthreads();
-    const int copies = VEC ? a.r_kv / 8 : a.r_kv;
-    const int items = copies + RopeItem<VEC>::count(a.rope.d_r);
-    for (int i = threadIdx.x; i < n * items; i += kAppendThreads) {
-        const int k = i / items, it = i % items;
-        if (dst_row[k] < 0) continue;
-        const T* c = (const T*)a.c + (tok0 + k) * a.c_stride;
-        T* y = (T*)a.cache + dst_row[k] * a.cache_stride;
-        if (it < copies) {
-            if constexpr (VEC) {
-                constexpr int kVecs = sizeof(T) / 2;  // 16-byte vectors of eight elements
+    const int lane = threadIdx.x & 31;
+    const int64_t tok0 = ((int64_t)blockIdx.x * (kAppendThreads / 32) + (threadIdx.x >> 5)) * a.per_warp;
+    if (tok0 >= a.nr.n) return;
+    const int n = (int)(a.nr.n - tok0 < a.per_warp ? a.nr.n - tok0 : a.per_warp);
+    constexpr int kAhead = 8;
+    RowItems it(lane, 32, VEC ? a.r_kv * (int)sizeof(T) / 16 : a.r_kv);
+    uint4 v[kAhead];
+    auto fetch = [&](RowItems from) {
 #pragma unroll
-                for (int v = 0; v < kVecs; ++v)
-                    reinterpret_cast<uint4*>(y + it * 8)[v] = reinterpret_cast<const uint4*>(c + it * 8)[v];
-            } else {
-                y[it] = c[it];
-            }
-        } else {
-            RopeItem<VEC> x(a.rope, it - copies);
-            x.load((const T*)a.k_r + (tok0 + k) * a.k_r_stride);
-            x.rotate(a.rope, position[k]);
-            x.store(y + a.r_kv);
+        for (int h = 0; h < kAhead; ++h) {
+            if (from.row < n) v[h] = reinterpret_cast<const uint4*>((const T*)a.c + (tok0 + from.row) * a.c_stride)[from.col];
+            from.next();
         }
+    };
+    if constexpr (VEC) fetch(it);  // (before the rows' places are known)
+    int64_t my_row = -1;
+    int32_t my_pos = 0;
+    if (lane < n) {
+        const int32_t tok = (int32_t)tok0 + lane, b = a.nr.seq_of(tok);
+        my_pos = a.nr.first_pos(b) + tok - a.nr.start[b];
+        if (my_pos >= a.rope.rows && a.rope.d_r > 0) append_error(a.status, 1);
+        else if (my_pos >= 0) my_row = checked_row(a.rows, b, my_pos, a.cache_rows, a.status);
+    }
+    auto row_of = [&](int k) { return __shfl_sync(0xffffffffu, my_row, k < n ? k : 0); };
+    if constexpr (VEC) {
+        for (int i0 = 0; i0 < n * it.per; i0 += 32 * kAhead) {
+            if (i0 > 0) fetch(it);
+#pragma unroll
+            for (int h = 0; h < kAhead; ++h) {
+                const int64_t row = row_of(it.row);
+                if (it.row < n && row >= 0) reinterpret_cast<uint4*>((T*)a.cache + row * a.cache_stride)[it.col] = v[h];
+                it.next();
+            }
+        }
+    } else {
+        for (int i0 = 0; i0 < n * it.per; i0 += 32) {
+            const int64_t row = row_of(it.row);
+            if (it.row < n && row >= 0)
+                ((T*)a.cache + row * a.cache_stride)[it.col] = ((const T*)a.c + (tok0 + it.row) * a.c_stride)[it.col];
+            it.next();
+        }
+    }
+    const int turns = RopeItem<VEC>::count(a.rope.d_r);
+    for (int i0 = 0; i0 < n * turns; i0 += 32) {
+        const int i = i0 + lane, k = turns > 0 ? i / turns : 0;
+        const int64_t row = row_of(k);
+        const int32_t pos = __shfl_sync(0xffffffffu, my_pos, k < n ? k : 0);
+        if (k >= n || row < 0) continue;
+        RopeItem<VEC> x(a.rope, i % turns);
+        x.load((const T*)a.k_r + (tok0 + k) * a.k_r_stride);
+        x.rotate(a.rope, pos);
+        x.store((T*)a.cache + row * a.cache_stride + a.r_kv);
     }
 }
 
@@ -251,6 +301,18 @@ __device__ __forceinline__ float pow2_scale(float amax, int least) {
     int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u);
     if (e < least) e = least;
     return __uint_as_float((uint32_t)(e + 127) << 23);
+}
+// Largest finite magnitude of eight bf16 values, as the 15 bits that order like it, kept in both halves of `m`.  (Infinities and NaN
+// are 0x7f80 and beyond; they are looked for only where the plain maximum says that there are some.)
+__device__ __forceinline__ uint32_t bf16_max(uint32_t m, const uint4& u) {
+    const uint32_t w[4] = {u.x & 0x7fff7fffu, u.y & 0x7fff7fffu, u.z & 0x7fff7fffu, u.w & 0x7fff7fffu};
+    uint32_t x = __vmaxu2(__vmaxu2(w[0], w[1]), __vmaxu2(w[2], w[3]));
+    if (__vcmpgeu2(x, 0x7f807f80u) != 0) {
+        x = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x = __vmaxu2(x, w[i] & __vcmpltu2(w[i], 0x7f807f80u));
+    }
+    return __vmaxu2(m, x);
 }
 __device__ __forceinline__ float finite_max(float m, float x) {
     const float a = fabsf(x);
@@ -279,47 +341,48 @@ struct AppendFp8Args {
     const int32_t* block_table;
     int32_t max_pages, page_size;
     int64_t kv_blocks;  // (unit, head) blocks; those behind rotate queries
+    int32_t unit_shift;  // k of the units, -1: by rows
     int32_t* status;
 };
 
-// A block takes one head of one page that gets new rows.  Unit u of sequence b is its page number u - unit0(b) from the first
-// touched one on, unit0(b) = start[b] / page + 2 b: a sequence with n new rows touches at most (n - 1) / page + 2 pages, and
-// successive unit0 are at least that far apart, so that no prefix sum over the sequences is needed; what is left over exits.
-// The rows' first kHeld chunks per thread stay in registers between the maximum and the coding (64 rows of the latent
-// cache are sixteen chunks a thread); larger pages read the rest again, from L1 or L2.
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(kAppendThreads) append_fp8_kernel(const AppendFp8Args a) {
-    constexpr int kWarps = kAppendThreads / 32;
+// A block takes one head of one page that gets new rows.  Units of pages, without a prefix sum over the sequences:
+//   by rows    unit u is new row u, if that is the first new one of its page (steps: fewer rows than the other bound)
+//   otherwise  unit u of sequence b is its page number u - unit0(b) from the first touched one on, unit0(b) = (start[b] >> k) + 2 b
+//              with 2^k <= page: n new rows touch at most (n - 1) / page + 2 pages, and successive unit0 are at least that far apart.
+// What is left over exits.
+// The first eight chunks of a thread stay in registers between the maximum and the coding: all of a page of 64 latent rows
+// with 512 threads, of 64 rows of one head of a plane with 128; larger pages read the rest again, from L1 or L2.  (256 threads with
+// sixteen chunks each left one block per SM: 20000 rows into the planes 205 us, a step of 64 rows 43.)
+constexpr int kLatentThreads = 512, kPlaneThreads = 128;
+template <typename T, bool VEC, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) append_fp8_kernel(const AppendFp8Args a) {
+    constexpr int kWarps = THREADS / 32;
     __shared__ float red[kWarps];
     tc::pdl_launch_dependents();
     tc::pdl_wait();
     if ((int64_t)blockIdx.x >= a.kv_blocks)
-        return rotate_queries<T, VEC>(a.nr, a.rope, a.q, ((int64_t)blockIdx.x - a.kv_blocks) * kAppendThreads + threadIdx.x, a.status);
+        return rotate_queries<T, VEC>(a.nr, a.rope, a.q, ((int64_t)blockIdx.x - a.kv_blocks) * THREADS + threadIdx.x, a.status);
     const int32_t unit = (int32_t)(blockIdx.x / a.heads_in_all);
     int head = (int)(blockIdx.x % a.heads_in_all);
     const int page = a.page_size;
-    int32_t b = 0;
-    {
-        int32_t hi = a.nr.B - 1;
-        while (b < hi) {
-            const int32_t mid = (b + hi + 1) >> 1;
-            if (a.nr.start[mid] / page + 2 * mid <= unit) b = mid;
-            else hi = mid - 1;
-        }
-    }
+    const int32_t b = a.unit_shift < 0 ? warp_last(a.nr.B, unit, [&](int32_t i) { return a.nr.start[i]; })
+                                       : warp_last(a.nr.B, unit, [&](int32_t i) { return (a.nr.start[i] >> a.unit_shift) + 2 * i; });
     const int32_t s0 = a.nr.start[b], n = a.nr.start[b + 1] - s0;
     const int32_t T_len = a.nr.seqlens[b], first = T_len - n;
     if (n <= 0 || T_len <= 0) return;
-    const int32_t k = (first > 0 ? first / page : 0) + unit - (s0 / page + 2 * b);  // page of the sequence
-    if (k < 0 || (int64_t)k * page >= T_len) return;
+    int32_t k;  // page of the sequence
+    if (a.unit_shift < 0) {
+        const int32_t pos = first + unit - s0;
+        if (pos < 0 || (unit != s0 && pos % page != 0)) return;
+        k = pos / page;
+    } else {
+        k = (first > 0 ? first / page : 0) + unit - ((s0 >> a.unit_shift) + 2 * b);
+        if (k < 0 || (int64_t)k * page >= T_len) return;
+    }
     const int32_t p0 = k * page;
     const int32_t lo = p0 > first ? p0 : first;  // new rows [lo, hi) of this page; first < p0 + page by the choice of k
     int32_t hi = T_len - p0 < page ? T_len : p0 + page;
-    const int32_t pid = k < a.max_pages ? a.block_table[(int64_t)b * a.max_pages + k] : -1;
-    if (pid < 0 || pid >= a.n_pages) {
-        if (threadIdx.x == 0) append_error(a.status, 2);
-        return;
-    }
+    const int32_t pid = k < a.max_pages ? a.block_table[(int64_t)b * a.max_pages + k] : -1;  // (looked at behind the loads of the rows)
     if (a.rope.d_r > 0 && hi > a.rope.rows) {  // rows behind the rotation table are left out
         if (threadIdx.x == 0) append_error(a.status, 1);
         hi = a.rope.rows;
@@ -331,51 +394,64 @@ __global__ void __launch_bounds__(kAppendThreads) append_fp8_kernel(const Append
     const T* src = (const T*)P.a + (int64_t)(s0 + lo - first) * P.a_stride + head * P.a_width;
     const T* rsrc = (const T*)a.k_r + (int64_t)(s0 + lo - first) * a.k_r_stride;
     const int width = P.a_width + (P.rope_heads ? a.rope.d_r : 0);
-    e4m3* page_dst = (e4m3*)P.dst + (int64_t)pid * page * P.dst_stride + (int64_t)head * width;
-    e4m3* dst = page_dst + (int64_t)(lo - p0) * P.dst_stride;
     const int rows = hi - lo;
     const int chunks = VEC ? P.a_width / 8 : P.a_width, turns = P.rope_heads ? RopeItem<VEC>::count(a.rope.d_r) : 0;
-    float* const scale_at = P.scale + (int64_t)pid * P.heads + head;
-    const float s_old = lo > p0 ? *scale_at : 0.f;  // the page's older rows, if it has any, hold it to this
     const int tid = threadIdx.x;
 
     // largest finite magnitude of the new rows
-    constexpr int kHeld = VEC && sizeof(T) == 2 ? 16 : 0;
+    constexpr int kHeld = VEC && sizeof(T) == 2 ? 8 : 0;
+    constexpr int kElems = VEC ? 8 : 1;
     uint4 held[kHeld > 0 ? kHeld : 1];
     float amax = 0.f;
-    const int a_items = rows * chunks;
+    const RowItems a0(tid, THREADS, chunks > 0 ? chunks : 1);
+    const int a_rows = chunks > 0 ? rows : 0;
     if constexpr (kHeld > 0) {
+        RowItems it = a0;
 #pragma unroll
         for (int h = 0; h < kHeld; ++h) {
-            const int i = tid + h * kAppendThreads;
-            if (i < a_items) held[h] = *reinterpret_cast<const uint4*>(src + (int64_t)(i / chunks) * P.a_stride + i % chunks * 8);
+            if (it.row < a_rows) held[h] = *reinterpret_cast<const uint4*>(src + (int64_t)it.row * P.a_stride + it.col * 8);
+            it.next();
         }
+    }
+    const RowItems r0(tid, THREADS, turns > 0 ? turns : 1);
+    const int r_rows = turns > 0 ? rows : 0;
+    if (pid < 0 || pid >= a.n_pages) {
+        if (tid == 0) append_error(a.status, 2);
+        return;
+    }
+    e4m3* page_dst = (e4m3*)P.dst + (int64_t)pid * page * P.dst_stride + (int64_t)head * width;
+    e4m3* dst = page_dst + (int64_t)(lo - p0) * P.dst_stride;
+    float* const scale_at = P.scale + (int64_t)pid * P.heads + head;
+    const float s_old = lo > p0 ? *scale_at : 0.f;  // the page's older rows, if it has any, hold it to this
+    {
+        RowItems it = a0;
+        if constexpr (kHeld > 0) {
+            uint32_t top = 0;
 #pragma unroll
-        for (int h = 0; h < kHeld; ++h)
-            if (tid + h * kAppendThreads < a_items) {
+            for (int h = 0; h < kHeld; ++h) {
+                if (it.row < a_rows) top = bf16_max(top, held[h]);
+                it.next();
+            }
+            amax = fmaxf(amax, __uint_as_float(__vmaxu2(top, top >> 16) << 16));
+        }
+        for (; it.row < a_rows; it.next()) {
+            const T* x = src + (int64_t)it.row * P.a_stride + it.col * kElems;
+            if constexpr (VEC) {
                 float v[8];
-                unpack8(held[h], v);
+                load8(x, v);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) amax = finite_max(amax, v[e]);
+            } else {
+                amax = finite_max(amax, ldf(x));
             }
-    }
-    for (int i = tid + kHeld * kAppendThreads; i < a_items; i += kAppendThreads) {
-        const T* x = src + (int64_t)(i / chunks) * P.a_stride + i % chunks * (VEC ? 8 : 1);
-        if constexpr (VEC) {
-            float v[8];
-            load8(x, v);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) amax = finite_max(amax, v[e]);
-        } else {
-            amax = finite_max(amax, ldf(x));
         }
-    }
-    for (int i = tid; i < rows * turns; i += kAppendThreads) {
-        RopeItem<VEC> x(a.rope, i % turns);
-        x.load(rsrc + (int64_t)(i / turns) * a.k_r_stride);
-        x.rotate(a.rope, lo + i / turns);
+        for (it = r0; it.row < r_rows; it.next()) {
+            RopeItem<VEC> x(a.rope, it.col);
+            x.load(rsrc + (int64_t)it.row * a.k_r_stride);
+            x.rotate(a.rope, lo + it.row);
 #pragma unroll
-        for (int e = 0; e < RopeItem<VEC>::kN; ++e) amax = finite_max(finite_max(amax, x.a[e]), x.b[e]);
+            for (int e = 0; e < RopeItem<VEC>::kN; ++e) amax = finite_max(finite_max(amax, x.a[e]), x.b[e]);
+        }
     }
     amax = warp_max(amax);
     if ((tid & 31) == 0) red[tid >> 5] = amax;
@@ -388,9 +464,8 @@ __global__ void __launch_bounds__(kAppendThreads) append_fp8_kernel(const Append
 
     if (lo > p0 && s > s_old) {  // the older rows under the larger scale
         const float ratio = s_old * inv;
-        const int per = VEC ? width / 8 : width;
-        for (int i = tid; i < (lo - p0) * per; i += kAppendThreads) {
-            e4m3* y = page_dst + (int64_t)(i / per) * P.dst_stride + i % per * (VEC ? 8 : 1);
+        for (RowItems it(tid, THREADS, VEC ? width / 8 : width); it.row < lo - p0; it.next()) {
+            e4m3* y = page_dst + (int64_t)it.row * P.dst_stride + it.col * kElems;
             if constexpr (VEC) {
                 const uint2 u = *reinterpret_cast<const uint2*>(y);
                 float v[8];
@@ -402,23 +477,23 @@ __global__ void __launch_bounds__(kAppendThreads) append_fp8_kernel(const Append
             }
         }
     }
+    RowItems it = a0;
     if constexpr (kHeld > 0) {
 #pragma unroll
         for (int h = 0; h < kHeld; ++h) {
-            const int i = tid + h * kAppendThreads;
-            if (i < a_items) {
+            if (it.row < a_rows) {
                 float v[8];
                 unpack8(held[h], v);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] *= inv;
-                store8(dst + (int64_t)(i / chunks) * P.dst_stride + i % chunks * 8, v);
+                store8(dst + (int64_t)it.row * P.dst_stride + it.col * 8, v);
             }
+            it.next();
         }
     }
-    for (int i = tid + kHeld * kAppendThreads; i < a_items; i += kAppendThreads) {
-        const int r = i / chunks, c = i % chunks * (VEC ? 8 : 1);
-        const T* x = src + (int64_t)r * P.a_stride + c;
-        e4m3* y = dst + (int64_t)r * P.dst_stride + c;
+    for (; it.row < a_rows; it.next()) {
+        const T* x = src + (int64_t)it.row * P.a_stride + it.col * kElems;
+        e4m3* y = dst + (int64_t)it.row * P.dst_stride + it.col * kElems;
         if constexpr (VEC) {
             float v[8];
             load8(x, v);
@@ -429,16 +504,16 @@ __global__ void __launch_bounds__(kAppendThreads) append_fp8_kernel(const Append
             stf(y, ldf(x) * inv);
         }
     }
-    for (int i = tid; i < rows * turns; i += kAppendThreads) {
-        RopeItem<VEC> x(a.rope, i % turns);
-        x.load(rsrc + (int64_t)(i / turns) * a.k_r_stride);
-        x.rotate(a.rope, lo + i / turns);
+    for (it = r0; it.row < r_rows; it.next()) {
+        RopeItem<VEC> x(a.rope, it.col);
+        x.load(rsrc + (int64_t)it.row * a.k_r_stride);
+        x.rotate(a.rope, lo + it.row);
 #pragma unroll
         for (int e = 0; e < RopeItem<VEC>::kN; ++e) {
             x.a[e] *= inv;
             x.b[e] *= inv;
         }
-        x.store(dst + (int64_t)(i / turns) * P.dst_stride + P.a_width);
+        x.store(dst + (int64_t)it.row * P.dst_stride + P.a_width);
     }
     if (tid == 0) *scale_at = s;
 }

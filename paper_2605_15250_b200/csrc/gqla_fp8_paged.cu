@@ -71,16 +71,24 @@ void fill(Args& k, const gqla_dims& d, const AppendCall& a) {
     k.k_r_stride = a.k_r_stride;
 }
 
-int64_t query_blocks(const gqla_dims& d, const AppendCall& a, bool vec) {
+int64_t query_blocks(const gqla_dims& d, const AppendCall& a, bool vec, int threads) {
     if (a.q_r == nullptr || d.d_r == 0) return 0;
     const int64_t items = a.n * d.h_q * (vec ? RopeItem<true>::count(d.d_r) : RopeItem<false>::count(d.d_r));
-    return (items + kAppendThreads - 1) / kAppendThreads;
+    return (items + threads - 1) / threads;
 }
 
 template <typename Args>
-gqla_status launch_append(void (*kern)(Args), const Args& a, int64_t blocks, cudaStream_t st) {
+gqla_status launch_append(void (*kern)(Args), const Args& a, int64_t blocks, int threads, cudaStream_t st) {
     if (blocks > 0x7fffffffLL) return GQLA_ERR_SHAPE;
-    return tc::launch_pdl(kern, dim3((unsigned)blocks), dim3(kAppendThreads), 0, st, a) == cudaSuccess ? GQLA_OK : GQLA_ERR_CUDA;
+    return tc::launch_pdl(kern, dim3((unsigned)blocks), dim3(threads), 0, st, a) == cudaSuccess ? GQLA_OK : GQLA_ERR_CUDA;
+}
+
+template <int THREADS>
+gqla_status launch_append_fp8_of(gqla_dtype dtype, bool vec, const AppendFp8Args& a, int64_t blocks, cudaStream_t st) {
+    if (dtype == GQLA_BF16)
+        return launch_append(vec ? append_fp8_kernel<__nv_bfloat16, true, THREADS> : append_fp8_kernel<__nv_bfloat16, false, THREADS>, a,
+                             blocks, THREADS, st);
+    return launch_append(vec ? append_fp8_kernel<float, true, THREADS> : append_fp8_kernel<float, false, THREADS>, a, blocks, THREADS, st);
 }
 
 gqla_status launch_append_fp8(const gqla_dims& d, const AppendCall& call, AppendFp8Args& a, bool vec, const int32_t* block_table,
@@ -89,13 +97,17 @@ gqla_status launch_append_fp8(const gqla_dims& d, const AppendCall& call, Append
     a.block_table = block_table; a.max_pages = max_pages; a.page_size = page_size; a.status = status_word;
     a.n_pages = (int32_t)(n_rows / page_size);
     a.heads_in_all = a.plane[0].heads + a.plane[1].heads + a.plane[2].heads;
-    const int64_t units = call.n / page_size + 2 * (int64_t)call.B;
+    int shift = 0;
+    while ((2 << shift) <= page_size) ++shift;
+    const int64_t by_pages = (call.n >> shift) + 2 * (int64_t)call.B;
+    const int64_t units = call.n < by_pages ? call.n : by_pages;
+    a.unit_shift = call.n < by_pages ? -1 : shift;
     if (units > 0x7fffffffLL) return GQLA_ERR_SHAPE;
     a.kv_blocks = units * a.heads_in_all;
-    const int64_t blocks = a.kv_blocks + query_blocks(d, call, vec);
-    if (call.dtype == GQLA_BF16)
-        return launch_append(vec ? append_fp8_kernel<__nv_bfloat16, true> : append_fp8_kernel<__nv_bfloat16, false>, a, blocks, st);
-    return launch_append(vec ? append_fp8_kernel<float, true> : append_fp8_kernel<float, false>, a, blocks, st);
+    const int threads = a.heads_in_all == 1 ? kLatentThreads : kPlaneThreads;
+    const int64_t blocks = a.kv_blocks + query_blocks(d, call, vec, threads);
+    return threads == kLatentThreads ? launch_append_fp8_of<kLatentThreads>(call.dtype, vec, a, blocks, st)
+                                     : launch_append_fp8_of<kPlaneThreads>(call.dtype, vec, a, blocks, st);
 }
 
 // ------------------------------------------------------------------------------------------------ attention
@@ -369,14 +381,17 @@ gqla_status gqla_append_rope(const gqla_dims* d, gqla_dtype dtype, int32_t B, in
     a.cache = cache; a.cache_stride = cache_row_stride; a.cache_rows = cache_rows;
     a.rows = block_table != nullptr ? RowMap{nullptr, block_table, max_pages, page_size} : RowMap{seq_start, nullptr, 0, 1};
     a.status = status_word;
-    a.per_block = n_new >= 4096 ? kAppendMostRows : 4;
-    const int64_t kv = (n_new + a.per_block - 1) / a.per_block;
+    // a row per warp while that does not fill the GPU, eight beyond (each lane then keeps eight loads in flight)
+    a.per_warp = n_new >= 8192 ? kAppendMostRows : 1;
+    const int64_t rows_per_block = (int64_t)a.per_warp * (kAppendThreads / 32);
+    const int64_t kv = (n_new + rows_per_block - 1) / rows_per_block;
     a.kv_blocks = (int32_t)kv;
-    const int64_t blocks = kv + query_blocks(*d, call, vec);
+    const int64_t blocks = kv + query_blocks(*d, call, vec, kAppendThreads);
     cudaStream_t st = (cudaStream_t)stream;
     if (dtype == GQLA_BF16)
-        return launch_append(vec ? append_rope_kernel<__nv_bfloat16, true> : append_rope_kernel<__nv_bfloat16, false>, a, blocks, st);
-    return launch_append(vec ? append_rope_kernel<float, true> : append_rope_kernel<float, false>, a, blocks, st);
+        return launch_append(vec ? append_rope_kernel<__nv_bfloat16, true> : append_rope_kernel<__nv_bfloat16, false>, a, blocks,
+                             kAppendThreads, st);
+    return launch_append(vec ? append_rope_kernel<float, true> : append_rope_kernel<float, false>, a, blocks, kAppendThreads, st);
 }
 
 gqla_status gqla_append_rope_fp8(const gqla_dims* d, gqla_dtype dtype, int32_t B, int64_t n_new, const int32_t* new_start,
