@@ -8,6 +8,7 @@
 #include "common.cuh"
 #include "sched.cuh"
 #include "tc_common.cuh"
+#include "tc_decode_fp8_pair.cuh"
 #include "tc_decode_fp8_paged.cuh"
 
 using namespace gqla;
@@ -238,7 +239,41 @@ bool covers(const gqla_dims& d, gqla_dtype dtype, int32_t s_q, int32_t page_size
            page_size % 16 == 0 && s_q <= 4096;
 }
 
+// Absorb path: CTA pairs with the query rows on M beyond 32 rows.  A pair does 128 rows of a tile in less time than the
+// tokens-on-M kernel's CTAs do 64 of them (64 x 4096 rows, 128 heads: 116 us there), which up to 32 rows is bound by HBM.
+bool on_pairs(const gqla_dims& d, int32_t s_q, bool latent) { return latent && (int64_t)s_q * d.h_q > 32; }
+
+// CTA pairs resident at once on the current device, 0 where it cannot be asked.
+int resident_pairs() {
+    static int cached[64] = {};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+    if (cached[dev] == 0) {
+        auto kern = tc::decode_fp8_pair_kernel<64>;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(2 * 148, 1, 1);
+        cfg.blockDim = dim3(tc::Fp8PairSmem::kThreads, 1, 1);
+        cfg.dynamicSmemBytes = tc::Fp8PairSmem::kTotal;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = 2;
+        attr[0].val.clusterDim.y = 1;
+        attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        int n = 0;
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, tc::Fp8PairSmem::kTotal) != cudaSuccess ||
+            cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess || n <= 0) {
+            (void)cudaGetLastError();
+            return 0;
+        }
+        cached[dev] = n;
+    }
+    return cached[dev];
+}
+
 int32_t workers_of(const gqla_dims& d, int32_t s_q, bool latent) {
+    if (on_pairs(d, s_q, latent)) return resident_pairs() / (int32_t)(((int64_t)s_q * d.h_q + 127) / 128);
     const RowBlocks r = row_blocks(s_q, latent ? d.h_q : d.h_q / d.g);
     const int64_t per = r.count() * (latent ? 1 : d.g);
     return per > 0 ? (int32_t)(sm_count() / per) : 0;
@@ -255,7 +290,43 @@ cudaError_t launch_tc(const tc::Fp8PagedParams& p, const CUtensorMap& k, const C
 }
 
 template <int PG>
+gqla_status tc_decode_fp8_pairs(const Fp8PagedCall& c, cudaStream_t st) {
+    const gqla_dims& d = *c.d;
+    const int64_t rows_total = (int64_t)c.s_q * d.h_q, row_blocks = (rows_total + 127) / 128;
+    const int32_t workers = c.S < 0 ? workers_of(d, c.s_q, true) : 0;
+    const bool balanced = workers > 0;
+    const int32_t S = c.S < 0 ? -c.S : c.S;
+    const int64_t pairs = (balanced ? (int64_t)workers : (int64_t)c.B * S) * row_blocks;
+    if (2 * pairs > 0x7fffffffLL || rows_total * c.B > 0x7fffffffLL) return GQLA_ERR_UNSUPPORTED;
+    CUtensorMap tmC, tmCr;
+    tc::CutMaps<PG> cut;
+    const uint64_t dims[2] = {(uint64_t)(d.r_kv + d.d_r), (uint64_t)c.n_rows}, str[1] = {(uint64_t)c.k_stride};
+    auto map = [&](CUtensorMap* m, uint32_t cols, uint32_t rows, CUtensorMapSwizzle swizzle) {
+        const uint32_t box[2] = {cols, rows};
+        return tc::make_tmap_u8(m, c.k, 2, dims, str, box, swizzle);
+    };
+    if (!map(&tmC, 128, PG, CU_TENSOR_MAP_SWIZZLE_128B) || !map(&tmCr, 64, PG, CU_TENSOR_MAP_SWIZZLE_64B) ||
+        !map(&cut.rows8, 128, 8, CU_TENSOR_MAP_SWIZZLE_128B) || !map(&cut.row1, 128, 1, CU_TENSOR_MAP_SWIZZLE_128B))
+        return GQLA_ERR_CUDA;
+    tc::Fp8PairParams p{};
+    p.B = c.B; p.S = S; p.s_q = c.s_q; p.h_q = d.h_q; p.rows_total = (int32_t)rows_total; p.row_blocks = (int32_t)row_blocks;
+    p.balanced = balanced ? 1 : 0; p.W = workers;
+    p.n_rows = (int32_t)c.n_rows; p.n_pages = (int32_t)(c.n_rows / c.page_size);
+    p.scale_log2 = c.scale * 1.4426950408889634f;
+    p.q = (const __nv_bfloat16*)c.q; p.page_scale = c.k_scale;
+    p.rows = RowMap{nullptr, c.block_table, c.max_pages, c.page_size};
+    p.seqlens = c.seqlens; p.o_part = c.o_part; p.lse_part = c.lse_part; p.status = c.status;
+    auto kern = tc::decode_fp8_pair_kernel<PG>;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, tc::Fp8PairSmem::kTotal) != cudaSuccess) return GQLA_ERR_CUDA;
+    return tc::launch_pdl(kern, dim3((unsigned)(2 * pairs)), dim3(tc::Fp8PairSmem::kThreads), tc::Fp8PairSmem::kTotal, st, p, tmC, tmCr,
+                          cut) == cudaSuccess
+               ? GQLA_OK
+               : GQLA_ERR_CUDA;
+}
+
+template <int PG>
 gqla_status tc_decode_fp8_paged(const Fp8PagedCall& c, cudaStream_t st) {
+    if (on_pairs(*c.d, c.s_q, c.latent)) return tc_decode_fp8_pairs<PG>(c, st);
     const gqla_dims& d = *c.d;
     const int g = c.latent ? 1 : d.g, heads = d.h_q / g;
     const RowBlocks rb = row_blocks(c.s_q, heads);

@@ -117,12 +117,13 @@ def test_decode_errors_of_one_path():
 
 def test_warps_of_the_paged_kernels_leave_by_vote():
     """Block barriers have no limit, so the warps that meet in them leave a loop together, by a vote on their failed waits."""
-    path = os.path.join(ROOT, "paper_2605_15250_b200", "csrc", "tc_decode_fp8_paged.cuh")
-    text = re.sub(r"//[^\n]*", "", open(path).read())
-    kernel = text.split("__global__")[1]
-    softmax = kernel.split("vote_any(")[0].rfind("} else {")
-    assert ".raised()" not in kernel[softmax:]
-    assert re.search(r"if \(vote_any\(\w+, !okl, [^;{]*\)\) \{ ok = false; break; \}", kernel)
+    for name in ("tc_decode_fp8_paged.cuh", "tc_decode_fp8_pair.cuh"):
+        path = os.path.join(ROOT, "paper_2605_15250_b200", "csrc", name)
+        text = re.sub(r"//[^\n]*", "", open(path).read())
+        kernel = text.split("__global__")[1]
+        softmax = kernel.split("vote_any(")[0].rfind("} else")
+        assert ".raised()" not in kernel[softmax:], name
+        assert re.search(r"if \(vote_any\(\w+, !okl, [^;{]*\)\) \{ ok = false; break; \}", kernel), name
 
 
 # ------------------------------------------------------------------ the oracle's statements
