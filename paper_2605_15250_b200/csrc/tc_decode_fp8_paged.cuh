@@ -164,6 +164,61 @@ __device__ __forceinline__ float rcp(float x) {
     return y;
 }
 
+// Eight bf16 query elements times `inv` (a power of two: at most 448) as two codes each, hi (nearest) and lo (nearest to the rest).  By
+// way of fp16, which holds the eight bits of what is not below 2^-14.
+__device__ __forceinline__ void split_query8(const uint4& u, float inv, uint2& hi, uint2& lo) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    uint16_t h[4], l[4];
+    const uint64_t inv2 = pack2(inv, inv);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float x0, x1;
+        unpack2(mul2(pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u)), inv2), x0, x1);
+        asm("{\n\t.reg .b32 h, b;\n\t"
+            "cvt.rn.f16x2.f32 h, %3, %2;\n\t"
+            "cvt.rn.satfinite.e4m3x2.f16x2 %0, h;\n\t"
+            "cvt.rn.f16x2.e4m3x2 b, %0;\n\t"
+            "sub.rn.f16x2 b, h, b;\n\t"
+            "cvt.rn.satfinite.e4m3x2.f16x2 %1, b;\n\t}"
+            : "=&h"(h[i]), "=h"(l[i])
+            : "f"(x0), "f"(x1));
+    }
+    hi = make_uint2((uint32_t)h[0] | ((uint32_t)h[1] << 16), (uint32_t)h[2] | ((uint32_t)h[3] << 16));
+    lo = make_uint2((uint32_t)l[0] | ((uint32_t)l[1] << 16), (uint32_t)l[2] | ((uint32_t)l[3] << 16));
+}
+// Two query rows of W bf16 elements in a warp, sixteen lanes each: fetched, scaled by a power of two and cut into two terms.
+template <int W>
+struct QueryPair {
+    static constexpr int kChunks = W / 8, kPer = (kChunks + 15) / 16;
+    uint4 u[kPer];
+    __device__ __forceinline__ void fetch(const __nv_bfloat16* row, bool valid, int lane) {
+#pragma unroll
+        for (int c = 0; c < kPer; ++c) {
+            const int ci = lane % 16 + 16 * c;
+            u[c] = valid && ci < kChunks ? reinterpret_cast<const uint4*>(row)[ci] : make_uint4(0, 0, 0, 0);
+        }
+    }
+    // Hands column 8 ci .. + 7's codes to store(first column, hi, lo); returns the row's scale.  sign: of the stored values.
+    template <typename F>
+    __device__ __forceinline__ float cut(int lane, float sign, F store) const {
+        uint32_t top = 0;
+#pragma unroll
+        for (int c = 0; c < kPer; ++c) top = bf16_max(top, u[c]);
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const float amax = __uint_as_float(__vmaxu2(top, top >> 16) << 16);
+        const float qs = amax > 0.f ? pow2_scale(amax, -110) : 1.f;
+        const float inv = copysignf(__uint_as_float((254u << 23) - __float_as_uint(qs)), sign);  // 1 / qs
+#pragma unroll
+        for (int c = 0; c < kPer; ++c) {
+            const int ci = lane % 16 + 16 * c;
+            uint2 hi, lo;
+            split_query8(u[c], inv, hi, lo);
+            if (ci < kChunks) store(ci * 8, hi, lo);
+        }
+        return qs;
+    }
+};
 // OR of a predicate over the `nthreads` threads that call it on named barrier `id`.  (Warps that meet in barriers leave a loop by
 // such a vote, tc_common.cuh.)
 __device__ __forceinline__ bool vote_any(int id, bool v, int nthreads) {
@@ -277,6 +332,10 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
             const int n_tiles = warp_uniform(pc.n_tiles);
             if (n_tiles == 0) continue;
             const int32_t T = p.seqlens[pc.b];
+            // the query rows, which the softmax warps read when they are through with the piece before: the heads of a position are together
+            if (lane < (R >> p.hshift) && pq0 + lane < p.s_q)
+                prefetch_l2(reinterpret_cast<const uint8_t*>(p.q + (((int64_t)pc.b * p.s_q + pq0 + lane) * p.h_q + (int64_t)j * p.hpg + i0) * kQWidth),
+                            (uint32_t)((p.hpg - i0 < p.hb ? p.hpg - i0 : p.hb) * kQWidth * 2));
             // This lane's run of the tile that is looked up next: its first token, that one's place in its page, the page's in the
             // block table.  Page numbers are looked up two tiles ahead, scales one.
             const int run = lane % NB;
@@ -496,55 +555,18 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
             if (pc.n_tiles > 0) {
                 // ---------------------------------------------------------- the piece's query rows, two a warp
                 // (the scores of the previous piece's last tile have been read, so nothing reads the old rows any more)
-                constexpr int kChunks = kQWidth / 8, kPer = (kChunks + 31) / 32;
-                uint4 u[2][kPer];
-#pragma unroll
-                for (int w = 0; w < 2; ++w) {
-                    const int r = sw + w * L::kSoftmaxWarps, pq = pq0 + (r >> p.hshift), il = i0 + (r & hmask);
-                    const bool valid = il < p.hpg && pq < p.s_q;
-                    const uint4* src = reinterpret_cast<const uint4*>(
-                        p.q + (((int64_t)pc.b * p.s_q + pq) * p.h_q + (int64_t)j * p.hpg + il) * kQWidth);
-#pragma unroll
-                    for (int c = 0; c < kPer; ++c)
-                        u[w][c] = valid && lane + 32 * c < kChunks ? src[lane + 32 * c] : make_uint4(0, 0, 0, 0);
-                }
-#pragma unroll
-                for (int w = 0; w < 2; ++w) {
-                    const int r = sw + w * L::kSoftmaxWarps;
-                    float amax = 0.f;
-#pragma unroll
-                    for (int c = 0; c < kPer; ++c) {
-                        float v[8];
-                        unpack8(u[w][c], v);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) amax = finite_max(amax, v[i]);
-                    }
-                    amax = warp_max(amax);
-                    const float qs = amax > 0.f ? pow2_scale(amax, -110) : 1.f, inv = 1.f / qs;
-#pragma unroll
-                    for (int c = 0; c < kPer; ++c) {
-                        const int ci = lane + 32 * c;
-                        float v[8];
-                        unpack8(u[w][c], v);
-                        uint32_t hi[4], lo[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float x0 = v[2 * i] * inv, x1 = v[2 * i + 1] * inv;
-                            hi[i] = float2_to_e4m3x2(x0, x1);
-                            lo[i] = float2_to_e4m3x2(x0 - e4m3_to_float((uint8_t)(hi[i] & 0xff)), x1 - e4m3_to_float((uint8_t)(hi[i] >> 8)));
-                        }
-                        // blocks of 128 columns: 128-byte rows, 16-byte chunks XORed with r % 8; the RoPE block: 64-byte rows, with r / 2 % 4
-                        const int col = ci * 8, blk = col / 128;
-                        const int pitch = blk < KB ? 128 : 64;
-                        uint8_t* at = q_smem + (blk < KB ? blk * L::kQBlock + ((((col % 128) >> 4) ^ (r & 7)) << 4)
-                                                         : KB * L::kQBlock + ((((col - KB * 128) >> 4) ^ ((r >> 1) & 3)) << 4)) + (col & 8);
-                        if (ci < kChunks) {
-                            *reinterpret_cast<uint2*>(at + L::qrow(r, 0) * pitch) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
-                            *reinterpret_cast<uint2*>(at + L::qrow(r, 1) * pitch) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
-                        }
-                    }
-                    if (lane == 0) sm_scale[r] = p.scale_log2 * qs;
-                }
+                const int r = 2 * sw + (lane >> 4), pq = pq0 + (r >> p.hshift), il = i0 + (r & hmask);
+                QueryPair<kQWidth> rows;
+                rows.fetch(p.q + (((int64_t)pc.b * p.s_q + pq) * p.h_q + (int64_t)j * p.hpg + il) * kQWidth, il < p.hpg && pq < p.s_q, lane);
+                const float qs = rows.cut(lane, 1.f, [&](int col, const uint2& hi, const uint2& lo) {
+                    // blocks of 128 columns: 128-byte rows, 16-byte chunks XORed with r % 8; the RoPE block: 64-byte rows, with r / 2 % 4
+                    const int blk = col / 128, pitch = blk < KB ? 128 : 64;
+                    uint8_t* at = q_smem + (blk < KB ? blk * L::kQBlock + ((((col % 128) >> 4) ^ (r & 7)) << 4)
+                                                     : KB * L::kQBlock + ((((col - KB * 128) >> 4) ^ ((r >> 1) & 3)) << 4)) + (col & 8);
+                    *reinterpret_cast<uint2*>(at + L::qrow(r, 0) * pitch) = hi;
+                    *reinterpret_cast<uint2*>(at + L::qrow(r, 1) * pitch) = lo;
+                });
+                if (lane % 16 == 0) sm_scale[r] = p.scale_log2 * qs;
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(q_full);

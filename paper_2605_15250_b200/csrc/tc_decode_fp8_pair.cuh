@@ -196,6 +196,10 @@ decode_fp8_pair_kernel(const Fp8PairParams p, const __grid_constant__ CUtensorMa
             const int n_tiles = warp_uniform(pc.n_tiles);
             if (n_tiles == 0) continue;
             const int32_t T = p.seqlens[pc.b];
+            // the query rows, which the softmax warps read when they are through with the piece before
+            if (lane == 0 && rho0 < p.rows_total)
+                prefetch_l2(reinterpret_cast<const uint8_t*>(p.q + ((int64_t)pc.b * p.rows_total + rho0) * 576),
+                            (uint32_t)(p.rows_total - rho0 < 64 ? p.rows_total - rho0 : 64) * 1152u);
             // a lane looks up a run of 16 tokens of the tile: page numbers two tiles ahead, scales one
             PageWalk pw(p.rows, pc.b, (uint32_t)(pc.tok_begin + (lane & 7) * 16), T);
             auto scale_of = [&](int32_t page) { return (uint32_t)page < (uint32_t)p.n_pages ? p.page_scale[page] : 1.f; };
@@ -401,9 +405,39 @@ decode_fp8_pair_kernel(const Fp8PairParams p, const __grid_constant__ CUtensorMa
         const uint32_t lane_base = tmem_base + ((uint32_t)(q * 32) << 16);
         const uint32_t p_ready_l[2] = {mapa(smem_u32(&p_ready[0]), 0), mapa(smem_u32(&p_ready[1]), 0)};
         const uint32_t o_free_l = mapa(smem_u32(o_free), 0), q_full_l = mapa(smem_u32(q_full), 0);
-        const int sw = warp - 2;
         const float scale_abs = fabsf(p.scale_log2);  // (a negative softmax scale turns the queries' signs)
         int gt = 0;  // tiles walked so far
+
+        // The query rows of a piece, eight a warp, a pair at a time with the next pair on its way.
+        auto write_q = [&]() {
+            // (the warp's number anew: what follows from it is not to be worked out ahead and kept in registers over the tiles)
+            int sw = warp - 2;
+            asm volatile("" : "+r"(sw));
+            auto fetch = [&](QueryPair<576>& rows, int i) {
+                const int rr = rho0 + sw * 8 + 2 * i + (lane >> 4);
+                rows.fetch(p.q + ((int64_t)pc.b * p.rows_total + rr) * 576, rr < p.rows_total, lane);
+            };
+            QueryPair<576> rows, ahead;
+            fetch(rows, 0);
+#pragma unroll 1
+            for (int i = 0; i < 4; ++i) {
+                if (i < 3) fetch(ahead, i + 1);
+                const int rl = sw * 8 + 2 * i + (lane >> 4);
+                const float qs = rows.cut(lane, p.scale_log2, [&](int col, const uint2& hi, const uint2& lo) {
+                    // boxes of 128 columns: 128-byte rows, 16-byte chunks XORed with r % 8; the RoPE box: 64-byte rows, with r / 2 % 4
+                    const int blk = col / 128;
+                    uint8_t* at = tiles + blk * L::kBox + (col & 8) +
+                                  (blk < 4 ? rl * 128 + ((((col % 128) >> 4) ^ (rl & 7)) << 4) : rl * 64 + ((((col - 512) >> 4) ^ ((rl >> 1) & 3)) << 4));
+                    *reinterpret_cast<uint2*>(at) = hi;
+                    *reinterpret_cast<uint2*>(at + L::kQTerm) = lo;
+                });
+                if (lane % 16 == 0) row_scale[rl] = scale_abs * qs;
+                rows = ahead;
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(q_full_l);
+        };
 
         while (walk.next(pc)) {
             GQLA_DEBUG_CHECK(pc.b >= 0 && pc.b < p.B, p.status, 32);  // a piece names a sequence of the batch
@@ -422,61 +456,8 @@ decode_fp8_pair_kernel(const Fp8PairParams p, const __grid_constant__ CUtensorMa
             if (lim > pc.tok_end) lim = pc.tok_end;
             lim -= pc.tok_begin;
             if (!row_valid) lim = 0;
-            if (pc.n_tiles > 0) {
-                // ---------------------------------------------------------- the piece's query rows, eight a warp
-                // (the scores of the previous piece's last tile have been read, so nothing reads the old rows any more)
-#pragma unroll 1
-                for (int i = 0; i < 8; i += 2) {
-                    uint4 u[2][3];
-#pragma unroll
-                    for (int w = 0; w < 2; ++w) {
-                        const int rr = rho0 + sw * 8 + i + w;
-                        const uint4* src = reinterpret_cast<const uint4*>(p.q + ((int64_t)pc.b * p.rows_total + rr) * 576);
-#pragma unroll
-                        for (int c = 0; c < 3; ++c)
-                            u[w][c] = rr < p.rows_total && lane + 32 * c < 72 ? src[lane + 32 * c] : make_uint4(0, 0, 0, 0);
-                    }
-#pragma unroll
-                    for (int w = 0; w < 2; ++w) {
-                        const int rl = sw * 8 + i + w;
-                        float amax = 0.f;
-#pragma unroll
-                        for (int c = 0; c < 3; ++c) {
-                            float v[8];
-                            unpack8(u[w][c], v);
-#pragma unroll
-                            for (int k2 = 0; k2 < 8; ++k2) amax = finite_max(amax, v[k2]);
-                        }
-                        amax = warp_max(amax);
-                        const float qs = amax > 0.f ? pow2_scale(amax, -110) : 1.f, inv = copysignf(1.f / qs, p.scale_log2);
-#pragma unroll
-                        for (int c = 0; c < 3; ++c) {
-                            const int ci = lane + 32 * c;
-                            float v[8];
-                            unpack8(u[w][c], v);
-                            uint32_t hi[4], lo[4];
-#pragma unroll
-                            for (int k2 = 0; k2 < 4; ++k2) {
-                                const float x0 = v[2 * k2] * inv, x1 = v[2 * k2 + 1] * inv;
-                                hi[k2] = float2_to_e4m3x2(x0, x1);
-                                lo[k2] = float2_to_e4m3x2(x0 - e4m3_to_float((uint8_t)(hi[k2] & 0xff)), x1 - e4m3_to_float((uint8_t)(hi[k2] >> 8)));
-                            }
-                            // boxes of 128 columns: 128-byte rows, 16-byte chunks XORed with r % 8; the RoPE box: 64-byte rows, with r / 2 % 4
-                            const int col = ci * 8, blk = col / 128;
-                            uint8_t* at = tiles + blk * L::kBox + (col & 8) +
-                                          (blk < 4 ? rl * 128 + ((((col % 128) >> 4) ^ (rl & 7)) << 4) : rl * 64 + ((((col - 512) >> 4) ^ ((rl >> 1) & 3)) << 4));
-                            if (ci < 72) {
-                                *reinterpret_cast<uint2*>(at) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
-                                *reinterpret_cast<uint2*>(at + L::kQTerm) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
-                            }
-                        }
-                        if (lane == 0) row_scale[rl] = scale_abs * qs;
-                    }
-                }
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(q_full_l);
-            }
+            // (the scores of the previous piece's last tile have been read, so nothing reads its rows any more)
+            if (pc.n_tiles > 0) write_q();
             named_bar_sync(1, L::kSoftmaxWarps * 32);  // the scales are there
             const float sl2 = row_scale[r];
             // m_used: the row's softmax REFERENCE (log2 units), the same in the four threads of the row: a raise puts it kAF8Bias
@@ -588,16 +569,18 @@ decode_fp8_pair_kernel(const Fp8PairParams p, const __grid_constant__ CUtensorMa
             }
 
             // -------------------------------------------------------------- epilogue: normalise and store
-            const int n_last = gt + pc.n_tiles - 1;
-            if (pc.n_tiles > 0 && ok)
+            const int n_tiles = pc.n_tiles;
+            const int64_t out_row = (slot0 + pc.k) * p.rows_total + rho;
+            sm_l[part * 64 + r] = l;
+            const int n_last = gt + n_tiles - 1;
+            if (n_tiles > 0 && ok)
                 ok = __all_sync(0xffffffffu, mbar_wait(&pv_done[n_last & 1], (n_last >> 1) & 1, ab, 9));
             tc_fence_after();
-            sm_l[part * 64 + r] = l;
             __syncwarp();
             if (lane == 0) mbar_arrive(fin);
             if (!__all_sync(0xffffffffu, mbar_wait(fin, pi & 1, ab, 11))) ok = false;
             const float Lt = (sm_l[r] + sm_l[64 + r]) + (sm_l[128 + r] + sm_l[192 + r]);
-            const bool live = ok && pc.n_tiles > 0 && Lt > 0.f && m_used > -INFINITY;
+            const bool live = ok && n_tiles > 0 && Lt > 0.f && m_used > -INFINITY;
             const float inv = live ? 1.f / Lt : 0.f;
             // The CTA's 64 output rows leave through shared memory (P and the V ring are idle now: the last
             // P.V has completed) as bulk stores.  The padded pitches keep the 16-byte stores of a quarter warp on
@@ -613,7 +596,7 @@ decode_fp8_pair_kernel(const Fp8PairParams p, const __grid_constant__ CUtensorMa
 #pragma unroll 1
                     for (int c = 0; c < 64; c += 32) {
                         uint32_t o[32];
-                        if (pc.n_tiles > 0 && ok) {  // warp-uniform
+                        if (n_tiles > 0 && ok) {  // warp-uniform
                             tmem_ld32(lane_base + kA8ColO + m * 128 + ch * 64 + c, o);
                             tmem_wait_ld();
                         }
@@ -631,7 +614,7 @@ decode_fp8_pair_kernel(const Fp8PairParams p, const __grid_constant__ CUtensorMa
                     }
                     fence_proxy_async_smem();  // staged row -> visible to the bulk-copy engine
                     if (row_valid && ok)
-                        bulk_store(p.o_part + ((slot0 + pc.k) * p.rows_total + rho) * 512 + 256 * m + 128 * hf + 64 * ch, own, 256);
+                        bulk_store(p.o_part + out_row * 512 + 256 * m + 128 * hf + 64 * ch, own, 256);
                     bulk_commit();
                     __syncwarp();
                 }
@@ -642,9 +625,9 @@ decode_fp8_pair_kernel(const Fp8PairParams p, const __grid_constant__ CUtensorMa
             if (lane == 0) mbar_arrive(epi_done);
             if (!__all_sync(0xffffffffu, mbar_wait(epi_done, pi & 1, ab, 12))) ok = false;
             if (row_valid && part == 0)
-                p.lse_part[(slot0 + pc.k) * p.rows_total + rho] =
+                p.lse_part[out_row] =
                     live ? (m_used + log2f(Lt)) * 0.6931471805599453f : -INFINITY;
-            gt += pc.n_tiles;
+            gt += n_tiles;
             ++pi;
         }
     }
