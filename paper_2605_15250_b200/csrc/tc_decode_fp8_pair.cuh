@@ -569,7 +569,7 @@ decode_fp8_pair_kernel(const Fp8PairParams p, const __grid_constant__ CUtensorMa
             }
 
             // -------------------------------------------------------------- epilogue: normalise and store
-            const int n_tiles = pc.n_tiles;
+            const int n_tiles = pc.n_tiles, out_k = pc.k;
             const int64_t out_row = (slot0 + pc.k) * p.rows_total + rho;
             sm_l[part * 64 + r] = l;
             const int n_last = gt + n_tiles - 1;
@@ -582,17 +582,16 @@ decode_fp8_pair_kernel(const Fp8PairParams p, const __grid_constant__ CUtensorMa
             const float Lt = (sm_l[r] + sm_l[64 + r]) + (sm_l[128 + r] + sm_l[192 + r]);
             const bool live = ok && n_tiles > 0 && Lt > 0.f && m_used > -INFINITY;
             const float inv = live ? 1.f / Lt : 0.f;
-            // The CTA's 64 output rows leave through shared memory (P and the V ring are idle now: the last
-            // P.V has completed) as bulk stores.  The padded pitches keep the 16-byte stores of a quarter warp on
+            // The output rows leave through shared memory (P and the V ring are idle now: the last P.V has completed): every warp turns 32
+            // rows x 64 columns of MMA m's block by itself and stores two rows of 256 bytes at a time.  (As bulk stores of 256 bytes, of
+            // which a CTA has 512, a piece's output took 8000 cycles.)  The padded pitch keeps the 16-byte accesses of a quarter warp on
             // distinct banks.
-            uint8_t* stage = tiles + L::kOffP;
             {
-                // fp32 partials: every warp stages and ships 32 rows x 64 columns of MMA m's block by itself (256-byte bulk
-                // stores), as in the bf16 kernel
-                uint8_t* own = stage + ((int)threadIdx.x - 64) * L::kWarpPitch;
+                uint8_t* own = tiles + L::kOffP + (warp - 2) * 32 * L::kWarpPitch;
+                const int64_t row0 = (slot0 + out_k) * p.rows_total + rho0 + (q & 1) * 32;  // the warp's first row
+                const int rows_left = p.rows_total - rho0 - (q & 1) * 32;
 #pragma unroll 1
                 for (int m = 0; m < 2; ++m) {
-                    if (m == 1) bulk_wait_read();  // this lane's row of m = 0 has left the staging
 #pragma unroll 1
                     for (int c = 0; c < 64; c += 32) {
                         uint32_t o[32];
@@ -602,7 +601,7 @@ decode_fp8_pair_kernel(const Fp8PairParams p, const __grid_constant__ CUtensorMa
                         }
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
-                            reinterpret_cast<float4*>(own)[c / 4 + i] =
+                            reinterpret_cast<float4*>(own + lane * L::kWarpPitch)[c / 4 + i] =
                                 live ? make_float4(__uint_as_float(o[4 * i]) * inv, __uint_as_float(o[4 * i + 1]) * inv,
                                                    __uint_as_float(o[4 * i + 2]) * inv, __uint_as_float(o[4 * i + 3]) * inv)
                                      : make_float4(0.f, 0.f, 0.f, 0.f);
@@ -612,15 +611,17 @@ decode_fp8_pair_kernel(const Fp8PairParams p, const __grid_constant__ CUtensorMa
                         __syncwarp();
                         if (lane == 0) mbar_arrive_cluster(o_free_l);
                     }
-                    fence_proxy_async_smem();  // staged row -> visible to the bulk-copy engine
-                    if (row_valid && ok)
-                        bulk_store(p.o_part + out_row * 512 + 256 * m + 128 * hf + 64 * ch, own, 256);
-                    bulk_commit();
+                    __syncwarp();
+                    float* out = p.o_part + row0 * 512 + 256 * m + 128 * hf + 64 * ch + (lane & 15) * 4;
+#pragma unroll 4
+                    for (int i = lane >> 4; i < 32; i += 2)
+                        if (i < rows_left && ok)
+                            *reinterpret_cast<float4*>(out + (int64_t)i * 512) = reinterpret_cast<const float4*>(own + i * L::kWarpPitch)[lane & 15];
                     __syncwarp();
                 }
-                bulk_wait_read();
             }
             // staging (and with it P and the V ring) is free again once every warp's stores have read it
+            fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(epi_done);
             if (!__all_sync(0xffffffffu, mbar_wait(epi_done, pi & 1, ab, 12))) ok = false;
