@@ -267,6 +267,50 @@ __device__ inline BalancedStart balanced_prepass(const int32_t* seqlens, int32_t
     __syncthreads();  // scratch may be reused by the caller
     return st;
 }
+
+// The balanced plan of the paged E4M3 kernels: as above, or one piece per sequence (sequence w to worker w, slots behind the first empty)
+// where there is about a sequence per worker and the longest is hardly longer than a share.  Cutting 64 sequences of 32 tiles into
+// 74 shares of 28 saves four tiles and costs nearly every worker a second piece, i.e. a second set of queries, first references and
+// outputs (absorb path, 128 heads, merge included: 83 us cut, 77 whole).  `slack`: tiles that a piece's start and end are worth.  Shares of
+// one tile are one piece each, so there the balanced plan has nothing to save.
+struct WholeOrBalanced {
+    Walker cut;
+    int32_t whole;  // this worker's sequence, -1: the balanced plan
+    bool done;
+    // All threads of the CTA call it; scratch and nthreads as for balanced_prepass.
+    __device__ void init_balanced(const int32_t* seqlens, int32_t B, int32_t S, int32_t w, int32_t W, int32_t slack, int32_t* scratch,
+                                  int nthreads) {
+        const BalancedStart st = balanced_prepass(seqlens, B, S, w, W, scratch, nthreads);
+        cut.init_balanced(seqlens, B, S, w, W, st);
+        whole = -1;
+        done = false;
+        if (B <= W && 2 * B > W) {
+            int32_t mx = 0;
+            for (int32_t i = threadIdx.x & 31; i < B; i += 32) mx = max(mx, tiles_of(seqlens[i]));
+            mx = __reduce_max_sync(0xffffffffu, mx);
+            if (st.share > 1 && mx <= st.share + slack) {
+                whole = w;
+                done = w >= B;
+            }
+        }
+    }
+    __device__ void init_fixed(const int32_t* seqlens, int32_t B, int32_t S, int32_t b, int32_t k) {
+        cut.init_fixed(seqlens, B, S, b, k);
+        whole = -1;
+        done = false;
+    }
+    __device__ bool next(Piece& pc) {
+        if (whole < 0) return cut.next(pc);
+        if (done) return false;
+        done = true;
+        const int32_t T = cut.seqlens[whole];
+        pc.b = whole; pc.k = 0;
+        pc.tok_begin = 0; pc.tok_end = T > 0 ? T : 0;
+        pc.n_tiles = tiles_of(T);
+        pc.fill_begin = pc.n_tiles > 0 ? 1 : 0; pc.fill_end = cut.S;
+        return true;
+    }
+};
 #endif
 
 }  // namespace gqla

@@ -309,10 +309,9 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
     const int unit = blockIdx.x / (p.row_blocks * p.g);
     const int i0 = rb % p.n_hb * p.hb;                  // first head of this row block in its group
     const int pq0 = rb / p.n_hb * (R >> p.hshift);      // first query position
-    Walker walk;
+    WholeOrBalanced walk;
     if (p.balanced) {
-        const BalancedStart st = balanced_prepass(p.seqlens, p.B, p.S, unit, p.W, reinterpret_cast<int32_t*>(red), L::kThreads);
-        walk.init_balanced(p.seqlens, p.B, p.S, unit, p.W, st);
+        walk.init_balanced(p.seqlens, p.B, p.S, unit, p.W, LATENT ? 3 : 6, reinterpret_cast<int32_t*>(red), L::kThreads);
     } else {
         walk.init_fixed(p.seqlens, p.B, p.S, unit / p.S, unit % p.S);
     }

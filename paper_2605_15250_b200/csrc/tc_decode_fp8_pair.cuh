@@ -172,11 +172,9 @@ decode_fp8_pair_kernel(const Fp8PairParams p, const __grid_constant__ CUtensorMa
     // the plan of this pair: row block rb, and either one (sequence, split) piece or worker w's share
     const int pair = blockIdx.x >> 1;
     const int rb = pair % p.row_blocks;
-    Walker walk;
+    WholeOrBalanced walk;
     if (p.balanced) {
-        const BalancedStart st = balanced_prepass(p.seqlens, p.B, p.S, pair / p.row_blocks, p.W,
-                                                  reinterpret_cast<int32_t*>(sm_max), L::kThreads);
-        walk.init_balanced(p.seqlens, p.B, p.S, pair / p.row_blocks, p.W, st);
+        walk.init_balanced(p.seqlens, p.B, p.S, pair / p.row_blocks, p.W, 6, reinterpret_cast<int32_t*>(sm_max), L::kThreads);
     } else {
         const int unit = pair / p.row_blocks;
         walk.init_fixed(p.seqlens, p.B, p.S, unit / p.S, unit % p.S);
