@@ -111,21 +111,39 @@ __device__ __forceinline__ void turn(float& a, float& b, float c, float s) {
     b = fmaf(x, s, b * c);
 }
 
-// A rotation item.  VEC: sixteen elements, item i of d_r / 16: the chunks 2 i and 2 i + 1, or i and i + d_r / 16 with halves.
-// Otherwise: one pair, item i of d_r / 2.
-template <bool VEC>
+// N = 4 or 8 of them.
+template <int N, typename T>
+__device__ __forceinline__ void load_n(const T* p, float* v) {
+    if constexpr (N == 8) {
+        load8(p, v);
+    } else if constexpr (sizeof(T) == 4) {
+        const float4 a = *reinterpret_cast<const float4*>(p);
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    } else {
+        const uint2 u = *reinterpret_cast<const uint2*>(p);
+        v[0] = __uint_as_float(u.x << 16); v[1] = __uint_as_float(u.x & 0xffff0000u);
+        v[2] = __uint_as_float(u.y << 16); v[3] = __uint_as_float(u.y & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void store4(e4m3* p, const float* v) {
+    *reinterpret_cast<uint32_t*>(p) = (uint32_t)float2_to_e4m3x2(v[0], v[1]) | ((uint32_t)float2_to_e4m3x2(v[2], v[3]) << 16);
+}
+
+// A rotation item: 2 N elements, item i of d_r / (2 N): N each from 2 N i and 2 N i + N on, or from N i and N i + d_r / 2 with halves.
+// N = 8 and 4 are vectors (4: half the registers, for pages), N = 1 a pair.
+template <int N>
 struct RopeItem {
-    static constexpr int kN = VEC ? 8 : 1;  // elements of each of the two parts
-    static __host__ __device__ int count(int d_r) { return VEC ? d_r / 16 : d_r / 2; }
+    static constexpr int kN = N;
+    static __host__ __device__ int count(int d_r) { return d_r / (2 * N); }
     float a[kN], b[kN];
     int ca, cb;  // first columns of the parts
     __device__ __forceinline__ RopeItem(const RopeTable& t, int i)
         : ca(t.halves ? i * kN : 2 * i * kN), cb(t.halves ? i * kN + t.d_r / 2 : (2 * i + 1) * kN) {}
     template <typename T>
     __device__ __forceinline__ void load(const T* x) {
-        if constexpr (VEC) {
-            load8(x + ca, a);
-            load8(x + cb, b);
+        if constexpr (N > 1) {
+            load_n<N>(x + ca, a);
+            load_n<N>(x + cb, b);
         } else {
             a[0] = ldf(x + ca);
             b[0] = ldf(x + cb);
@@ -134,32 +152,33 @@ struct RopeItem {
     __device__ __forceinline__ void rotate(const RopeTable& t, int32_t pos) {
         const float* cs = t.cs + (int64_t)pos * t.d_r;
         const int half = t.d_r / 2;
-        if constexpr (VEC) {
-            float c[8], s[8];
+        const int f = t.halves ? ca : ca / 2;
+        if constexpr (N > 1) {
+            float c[N], s[N];
+            load_n<N>(cs + f, c);
+            load_n<N>(cs + half + f, s);
             if (t.halves) {
-                load8(cs + ca, c);
-                load8(cs + half + ca, s);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) turn(a[k], b[k], c[k], s[k]);
-            } else {  // pairs within each part: frequencies ca / 2 .. ca / 2 + 7 over both
-                load8(cs + ca / 2, c);
-                load8(cs + half + ca / 2, s);
+                for (int k = 0; k < N; ++k) turn(a[k], b[k], c[k], s[k]);
+            } else {  // pairs within each part: N frequencies over both
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
+                for (int k = 0; k < N / 2; ++k) {
                     turn(a[2 * k], a[2 * k + 1], c[k], s[k]);
-                    turn(b[2 * k], b[2 * k + 1], c[4 + k], s[4 + k]);
+                    turn(b[2 * k], b[2 * k + 1], c[N / 2 + k], s[N / 2 + k]);
                 }
             }
         } else {
-            const int f = t.halves ? ca : ca / 2;
             turn(a[0], b[0], cs[f], cs[half + f]);
         }
     }
     template <typename T>
     __device__ __forceinline__ void store(T* y) const {
-        if constexpr (VEC) {
+        if constexpr (N == 8) {
             store8(y + ca, a);
             store8(y + cb, b);
+        } else if constexpr (N == 4) {
+            store4(y + ca, a);
+            store4(y + cb, b);
         } else {
             stf(y + ca, a[0]);
             stf(y + cb, b[0]);
@@ -170,14 +189,14 @@ struct RopeItem {
 // The queries' share of a launch: item index `i` counts (row, head, rotation item).
 template <typename T, bool VEC>
 __device__ __forceinline__ void rotate_queries(const NewRows& nr, const RopeTable& rope, const QueryRows& q, int64_t i, int32_t* status) {
-    const int per = RopeItem<VEC>::count(rope.d_r);
+    const int per = RopeItem<VEC ? 8 : 1>::count(rope.d_r);
     if (i >= nr.n * q.h_q * per) return;
     const int item = (int)(i % per), head = (int)(i / per % q.h_q);
     const int32_t tok = (int32_t)(i / per / q.h_q);
     const int32_t b = nr.seq_of(tok), pos = nr.first_pos(b) + tok - nr.start[b];
     if (pos < 0) return;
     if (pos >= rope.rows) return append_error(status, 1);
-    RopeItem<VEC> x(rope, item);
+    RopeItem<VEC ? 8 : 1> x(rope, item);
     x.load((const T*)q.src + tok * q.src_tok + head * q.src_head);
     x.rotate(rope, pos);
     x.store((T*)q.dst + tok * q.dst_tok + head * q.dst_head);
@@ -198,6 +217,16 @@ __device__ __forceinline__ int64_t checked_row(const RowMap& rows, int32_t b, in
     return -1;
 }
 
+// i / per for 0 <= i < 2^10 by a multiplication with m = ceil(2^32 / per): exact while i (m per - 2^32) < 2^32, which holds for
+// per < 2^22, and i < per beyond.
+struct ItemsOfRow {
+    int32_t per;
+    uint32_t recip;  // m; 0: per is 1
+    ItemsOfRow() = default;
+    explicit ItemsOfRow(int32_t per_) : per(per_), recip(per_ > 1 ? (uint32_t)(((1ull << 32) + (uint32_t)per_ - 1) / (uint32_t)per_) : 0u) {}
+    __device__ __forceinline__ int quotient(int i) const { return recip != 0 ? (int)__umulhi((uint32_t)i, recip) : i; }
+};
+
 struct AppendArgs {
     NewRows nr;
     RopeTable rope;
@@ -209,6 +238,7 @@ struct AppendArgs {
     int64_t cache_stride, cache_rows;
     RowMap rows;
     int32_t per_warp, kv_blocks;  // new rows of a warp; blocks behind kv_blocks rotate queries
+    ItemsOfRow items;             // vectors or elements of a latent part
     int32_t* status;
 };
 
@@ -217,8 +247,8 @@ constexpr int kAppendMostRows = 8;  // new rows of a warp
 // Item i, i + step, i + 2 step, .. of rows of `per` items each, without a division per item.
 struct RowItems {
     int row, col, row_step, col_step, per;
-    __device__ __forceinline__ RowItems(int i, int step, int per_)
-        : row(i / per_), col(i % per_), row_step(step / per_), col_step(step % per_), per(per_) {}
+    __device__ __forceinline__ RowItems(int i, int step, const ItemsOfRow& of)
+        : row(of.quotient(i)), col(i - row * of.per), row_step(of.quotient(step)), col_step(step - row_step * of.per), per(of.per) {}
     __device__ __forceinline__ void next() {
         row += row_step;
         col += col_step;
@@ -230,7 +260,7 @@ struct RowItems {
 };
 
 // A warp takes per_warp new rows: their places are looked up by a lane each, the latent parts copied eight 16-byte vectors a lane
-// at a time (49000 rows of 1152 bytes: 41.7 us with a block per sixteen rows and one vector a thread in flight), the RoPE parts rotated an
+// at a time (49000 rows of 1152 bytes: 25.9 us, 5.3 TB/s; 41.7 with a block per sixteen rows and one vector a thread in flight), the RoPE parts rotated an
 // item a lane.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kAppendThreads) append_rope_kernel(const AppendArgs a) {
@@ -243,7 +273,7 @@ __global__ void __launch_bounds__(kAppendThreads) append_rope_kernel(const Appen
     if (tok0 >= a.nr.n) return;
     const int n = (int)(a.nr.n - tok0 < a.per_warp ? a.nr.n - tok0 : a.per_warp);
     constexpr int kAhead = 8;
-    RowItems it(lane, 32, VEC ? a.r_kv * (int)sizeof(T) / 16 : a.r_kv);
+    RowItems it(lane, 32, a.items);
     uint4 v[kAhead];
     auto fetch = [&](RowItems from) {
 #pragma unroll
@@ -280,13 +310,13 @@ __global__ void __launch_bounds__(kAppendThreads) append_rope_kernel(const Appen
             it.next();
         }
     }
-    const int turns = RopeItem<VEC>::count(a.rope.d_r);
+    const int turns = RopeItem<VEC ? 8 : 1>::count(a.rope.d_r);
     for (int i0 = 0; i0 < n * turns; i0 += 32) {
         const int i = i0 + lane, k = turns > 0 ? i / turns : 0;
         const int64_t row = row_of(k);
         const int32_t pos = __shfl_sync(0xffffffffu, my_pos, k < n ? k : 0);
         if (k >= n || row < 0) continue;
-        RopeItem<VEC> x(a.rope, i % turns);
+        RopeItem<VEC ? 8 : 1> x(a.rope, i % turns);
         x.load((const T*)a.k_r + (tok0 + k) * a.k_r_stride);
         x.rotate(a.rope, pos);
         x.store((T*)a.cache + row * a.cache_stride + a.r_kv);
@@ -302,21 +332,37 @@ __device__ __forceinline__ float pow2_scale(float amax, int least) {
     if (e < least) e = least;
     return __uint_as_float((uint32_t)(e + 127) << 23);
 }
-// Largest finite magnitude of eight bf16 values, as the 15 bits that order like it, kept in both halves of `m`.  (Infinities and NaN
-// are 0x7f80 and beyond; they are looked for only where the plain maximum says that there are some.)
+// Largest magnitude of bf16 values, a running maximum in each half of `m` (signs of no meaning).  A NaN beside a number is passed over.
 __device__ __forceinline__ uint32_t bf16_max(uint32_t m, const uint4& u) {
-    const uint32_t w[4] = {u.x & 0x7fff7fffu, u.y & 0x7fff7fffu, u.z & 0x7fff7fffu, u.w & 0x7fff7fffu};
-    uint32_t x = __vmaxu2(__vmaxu2(w[0], w[1]), __vmaxu2(w[2], w[3]));
-    if (__vcmpgeu2(x, 0x7f807f80u) != 0) {
-        x = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x = __vmaxu2(x, w[i] & __vcmpltu2(w[i], 0x7f807f80u));
+    auto max2 = [](uint32_t a, uint32_t b) {
+        uint32_t r;
+        asm("max.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    };
+    return max2(m, max2(max2(u.x, u.y), max2(u.z, u.w)));
+}
+// The largest finite magnitude, from that maximum: where it is an infinity, `each` hands all chunks again.
+template <typename F>
+__device__ __forceinline__ float bf16_finite_max(uint32_t m, F each) {
+    m &= 0x7fff7fffu;
+    if (__vcmpgeu2(m, 0x7f807f80u) != 0) {
+        m = 0;
+        each([&](const uint4& u) {
+            const uint32_t w[4] = {u.x & 0x7fff7fffu, u.y & 0x7fff7fffu, u.z & 0x7fff7fffu, u.w & 0x7fff7fffu};
+            for (int i = 0; i < 4; ++i) m = __vmaxu2(m, w[i] & __vcmpltu2(w[i], 0x7f807f80u));
+        });
     }
-    return __vmaxu2(m, x);
+    return __uint_as_float(max(m & 0xffffu, m >> 16) << 16);
 }
 __device__ __forceinline__ float finite_max(float m, float x) {
     const float a = fabsf(x);
     return a <= FLT_MAX && a > m ? a : m;
+}
+
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
 }
 
 struct Fp8Plane {
@@ -328,6 +374,7 @@ struct Fp8Plane {
     int64_t dst_stride;
     float* scale;  // [pages, heads]
     int32_t heads;
+    ItemsOfRow copied, turned, coded;  // vectors or elements of the first part, rotation items, vectors or elements of a row of codes
 };
 
 struct AppendFp8Args {
@@ -342,6 +389,7 @@ struct AppendFp8Args {
     int32_t max_pages, page_size;
     int64_t kv_blocks;  // (unit, head) blocks; those behind rotate queries
     int32_t unit_shift;  // k of the units, -1: by rows
+    int32_t held;        // chunks of a thread that its shared memory has room for
     int32_t* status;
 };
 
@@ -350,20 +398,28 @@ struct AppendFp8Args {
 //   otherwise  unit u of sequence b is its page number u - unit0(b) from the first touched one on, unit0(b) = (start[b] >> k) + 2 b
 //              with 2^k <= page: n new rows touch at most (n - 1) / page + 2 pages, and successive unit0 are at least that far apart.
 // What is left over exits.
-// The first eight chunks of a thread stay in registers between the maximum and the coding: all of a page of 64 latent rows
-// with 512 threads, of 64 rows of one head of a plane with 128; larger pages read the rest again, from L1 or L2.  (256 threads with
-// sixteen chunks each left one block per SM: 20000 rows into the planes 205 us, a step of 64 rows 43.)
-constexpr int kLatentThreads = 512, kPlaneThreads = 128;
+// The first sixteen chunks of a thread stay in its shared memory between the maximum and the coding: all of a page of 64 latent rows
+// with 256 threads, of 64 rows of one head of a plane with 64; larger pages read the rest again, from L1 or L2.  They come by
+// asynchronous copies, which cost no registers while they are on their way.  Few warps of many chunks, since looking the unit up costs
+// each warp some 400 instructions.  49000 latent rows and 20000 rows into the planes: 27.6 and 34.6 us (3.7 and 4.2 TB/s); twice the threads
+// with eight chunks each 31.4 and 39.0, those chunks in registers 40.0 and 43.4.
+constexpr int kLatentThreads = 256, kPlaneThreads = 64;
 template <typename T, bool VEC, int THREADS>
-__global__ void __launch_bounds__(THREADS, 1024 / THREADS) append_fp8_kernel(const AppendFp8Args a) {
+struct HeldChunks {
+    static constexpr int kPer = VEC && sizeof(T) == 2 ? 16 : 0;  // most of a thread
+    static constexpr int kBytes = THREADS * 16;                 // of one each
+};
+template <typename T, bool VEC, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == kLatentThreads ? 3 : 16) append_fp8_kernel(const AppendFp8Args a) {
+    extern __shared__ uint4 append_held[];
     constexpr int kWarps = THREADS / 32;
     __shared__ float red[kWarps];
     tc::pdl_launch_dependents();
     tc::pdl_wait();
     if ((int64_t)blockIdx.x >= a.kv_blocks)
         return rotate_queries<T, VEC>(a.nr, a.rope, a.q, ((int64_t)blockIdx.x - a.kv_blocks) * THREADS + threadIdx.x, a.status);
-    const int32_t unit = (int32_t)(blockIdx.x / a.heads_in_all);
-    int head = (int)(blockIdx.x % a.heads_in_all);
+    const int32_t unit = THREADS == kLatentThreads ? (int32_t)blockIdx.x : (int32_t)(blockIdx.x / (unsigned)a.heads_in_all);
+    int head = (int)(blockIdx.x - (unsigned)unit * (unsigned)a.heads_in_all);
     const int page = a.page_size;
     const int32_t b = a.unit_shift < 0 ? warp_last(a.nr.B, unit, [&](int32_t i) { return a.nr.start[i]; })
                                        : warp_last(a.nr.B, unit, [&](int32_t i) { return (a.nr.start[i] >> a.unit_shift) + 2 * i; });
@@ -389,68 +445,100 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) append_fp8_kernel(con
         if (hi <= lo) return;
     }
     int pl = 0;
-    while (head >= a.plane[pl].heads) head -= a.plane[pl++].heads;
+    if constexpr (THREADS == kPlaneThreads) {  // (latent rows: one plane of one head, fields at fixed places)
+        while (head >= a.plane[pl].heads) head -= a.plane[pl++].heads;
+    } else {
+        head = 0;
+    }
     const Fp8Plane& P = a.plane[pl];
     const T* src = (const T*)P.a + (int64_t)(s0 + lo - first) * P.a_stride + head * P.a_width;
     const T* rsrc = (const T*)a.k_r + (int64_t)(s0 + lo - first) * a.k_r_stride;
     const int width = P.a_width + (P.rope_heads ? a.rope.d_r : 0);
     const int rows = hi - lo;
-    const int chunks = VEC ? P.a_width / 8 : P.a_width, turns = P.rope_heads ? RopeItem<VEC>::count(a.rope.d_r) : 0;
     const int tid = threadIdx.x;
 
     // largest finite magnitude of the new rows
-    constexpr int kHeld = VEC && sizeof(T) == 2 ? 8 : 0;
+    constexpr int kHeld = HeldChunks<T, VEC, THREADS>::kPer;
     constexpr int kElems = VEC ? 8 : 1;
-    uint4 held[kHeld > 0 ? kHeld : 1];
     float amax = 0.f;
-    const RowItems a0(tid, THREADS, chunks > 0 ? chunks : 1);
-    const int a_rows = chunks > 0 ? rows : 0;
-    if constexpr (kHeld > 0) {
-        RowItems it = a0;
-#pragma unroll
-        for (int h = 0; h < kHeld; ++h) {
-            if (it.row < a_rows) held[h] = *reinterpret_cast<const uint4*>(src + (int64_t)it.row * P.a_stride + it.col * 8);
-            it.next();
+    const RowItems a0(tid, THREADS, P.copied);
+    const int a_rows = P.a_width > 0 ? rows : 0;
+    // Calls f(h, offset) for the held chunks, offset in elements for rows of `stride`; leaves `rest` at the first that is not held.
+    RowItems rest = a0;
+    auto each_held = [&](int64_t stride, auto f) {
+        if (a0.col_step == 0) {  // one column per thread
+            int64_t off = a0.row * stride + a0.col * 8;
+            const int64_t step = a0.row_step * stride;
+            int row = a0.row;
+#pragma unroll 4
+            for (int h = 0; h < a.held; ++h, row += a0.row_step, off += step)
+                if (row < a_rows) f(h, off);
+            rest.row = row;
+        } else {
+            rest = a0;
+#pragma unroll 1
+            for (int h = 0; h < a.held; ++h, rest.next())
+                if (rest.row < a_rows) f(h, rest.row * stride + rest.col * 8);
         }
+    };
+    uint4* const held = append_held + tid;
+    if constexpr (kHeld > 0) {
+        each_held(P.a_stride, [&](int h, int64_t off) {
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(tc::smem_u32(held + h * THREADS)), "l"(src + off) : "memory");
+        });
     }
-    const RowItems r0(tid, THREADS, turns > 0 ? turns : 1);
-    const int r_rows = turns > 0 ? rows : 0;
+    const RowItems r0(tid, THREADS, P.turned);
+    const int r_rows = P.rope_heads ? rows : 0;
     if (pid < 0 || pid >= a.n_pages) {
         if (tid == 0) append_error(a.status, 2);
+        if constexpr (kHeld > 0) asm volatile("cp.async.wait_all;" ::: "memory");
         return;
     }
     e4m3* page_dst = (e4m3*)P.dst + (int64_t)pid * page * P.dst_stride + (int64_t)head * width;
     e4m3* dst = page_dst + (int64_t)(lo - p0) * P.dst_stride;
     float* const scale_at = P.scale + (int64_t)pid * P.heads + head;
     const float s_old = lo > p0 ? *scale_at : 0.f;  // the page's older rows, if it has any, hold it to this
-    {
-        RowItems it = a0;
-        if constexpr (kHeld > 0) {
-            uint32_t top = 0;
+    using Turn = RopeItem<VEC ? 4 : 1>;
+    auto turned = [&](const RowItems& it) {
+        Turn x(a.rope, it.col);
+        x.load(rsrc + (int64_t)it.row * a.k_r_stride);
+        x.rotate(a.rope, lo + it.row);
+        return x;
+    };
+    auto turned_max = [&](const Turn& x) {
 #pragma unroll
-            for (int h = 0; h < kHeld; ++h) {
-                if (it.row < a_rows) top = bf16_max(top, held[h]);
-                it.next();
-            }
-            amax = fmaxf(amax, __uint_as_float(__vmaxu2(top, top >> 16) << 16));
-        }
-        for (; it.row < a_rows; it.next()) {
-            const T* x = src + (int64_t)it.row * P.a_stride + it.col * kElems;
-            if constexpr (VEC) {
-                float v[8];
-                load8(x, v);
+        for (int e = 0; e < Turn::kN; ++e) amax = finite_max(finite_max(amax, x.a[e]), x.b[e]);
+    };
+    // of latent rows the first two items stay in registers: all of a page of 64.  (In the planes one block of 2 g + 1 has any.)
+    constexpr bool kHoldTurned = THREADS == kLatentThreads;
+    RowItems r1 = r0;
+    r1.next();
+    RowItems r2 = r0;
+    Turn t0(a.rope, r0.col), t1(a.rope, r1.col);
+    if constexpr (kHoldTurned) {
+        r2 = r1;
+        r2.next();
+        if (r0.row < r_rows) t0 = turned(r0);
+        if (r1.row < r_rows) t1 = turned(r1);
+        if (r0.row < r_rows) turned_max(t0);
+        if (r1.row < r_rows) turned_max(t1);
+    }
+    for (RowItems it = r2; it.row < r_rows; it.next()) turned_max(turned(it));
+    if constexpr (kHeld > 0) {
+        asm volatile("cp.async.wait_all;" ::: "memory");  // (a thread reads back what it has copied itself)
+        uint32_t top = 0;
+        each_held(0, [&](int h, int64_t) { top = bf16_max(top, held[h * THREADS]); });
+        amax = fmaxf(amax, bf16_finite_max(top, [&](auto f) { each_held(0, [&](int h, int64_t) { f(held[h * THREADS]); }); }));
+    }
+    for (RowItems it = rest; it.row < a_rows; it.next()) {
+        const T* x = src + (int64_t)it.row * P.a_stride + it.col * kElems;
+        if constexpr (VEC) {
+            float v[8];
+            load8(x, v);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) amax = finite_max(amax, v[e]);
-            } else {
-                amax = finite_max(amax, ldf(x));
-            }
-        }
-        for (it = r0; it.row < r_rows; it.next()) {
-            RopeItem<VEC> x(a.rope, it.col);
-            x.load(rsrc + (int64_t)it.row * a.k_r_stride);
-            x.rotate(a.rope, lo + it.row);
-#pragma unroll
-            for (int e = 0; e < RopeItem<VEC>::kN; ++e) amax = finite_max(finite_max(amax, x.a[e]), x.b[e]);
+            for (int e = 0; e < 8; ++e) amax = finite_max(amax, v[e]);
+        } else {
+            amax = finite_max(amax, ldf(x));
         }
     }
     amax = warp_max(amax);
@@ -461,10 +549,11 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) append_fp8_kernel(con
     const float need = pow2_scale(amax, kSmallestScaleExp);
     const float s = need > s_old ? need : s_old;
     const float inv = 1.f / s;
+    const uint32_t inv2 = tc::pack_bf16(inv, inv);
 
     if (lo > p0 && s > s_old) {  // the older rows under the larger scale
         const float ratio = s_old * inv;
-        for (RowItems it(tid, THREADS, VEC ? width / 8 : width); it.row < lo - p0; it.next()) {
+        for (RowItems it(tid, THREADS, P.coded); it.row < lo - p0; it.next()) {
             e4m3* y = page_dst + (int64_t)it.row * P.dst_stride + it.col * kElems;
             if constexpr (VEC) {
                 const uint2 u = *reinterpret_cast<const uint2*>(y);
@@ -477,21 +566,17 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) append_fp8_kernel(con
             }
         }
     }
-    RowItems it = a0;
     if constexpr (kHeld > 0) {
-#pragma unroll
-        for (int h = 0; h < kHeld; ++h) {
-            if (it.row < a_rows) {
-                float v[8];
-                unpack8(held[h], v);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] *= inv;
-                store8(dst + (int64_t)it.row * P.dst_stride + it.col * 8, v);
-            }
-            it.next();
-        }
+        each_held(P.dst_stride, [&](int h, int64_t off) {
+            // times the power of two in bf16: exact but for values below 2^-126, whose codes are zero
+            uint4 u = held[h * THREADS];
+            u = make_uint4(mul_bf16x2(u.x, inv2), mul_bf16x2(u.y, inv2), mul_bf16x2(u.z, inv2), mul_bf16x2(u.w, inv2));
+            float v[8];
+            unpack8(u, v);
+            store8(dst + off, v);
+        });
     }
-    for (; it.row < a_rows; it.next()) {
+    for (RowItems it = rest; it.row < a_rows; it.next()) {
         const T* x = src + (int64_t)it.row * P.a_stride + it.col * kElems;
         e4m3* y = dst + (int64_t)it.row * P.dst_stride + it.col * kElems;
         if constexpr (VEC) {
@@ -504,16 +589,21 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) append_fp8_kernel(con
             stf(y, ldf(x) * inv);
         }
     }
-    for (it = r0; it.row < r_rows; it.next()) {
-        RopeItem<VEC> x(a.rope, it.col);
-        x.load(rsrc + (int64_t)it.row * a.k_r_stride);
-        x.rotate(a.rope, lo + it.row);
+    auto store_turned = [&](Turn& x, int row) {
 #pragma unroll
-        for (int e = 0; e < RopeItem<VEC>::kN; ++e) {
+        for (int e = 0; e < Turn::kN; ++e) {
             x.a[e] *= inv;
             x.b[e] *= inv;
         }
-        x.store(dst + (int64_t)it.row * P.dst_stride + P.a_width);
+        x.store(dst + (int64_t)row * P.dst_stride + P.a_width);
+    };
+    if constexpr (kHoldTurned) {
+        if (r0.row < r_rows) store_turned(t0, r0.row);
+        if (r1.row < r_rows) store_turned(t1, r1.row);
+    }
+    for (RowItems it = r2; it.row < r_rows; it.next()) {
+        Turn x = turned(it);
+        store_turned(x, it.row);
     }
     if (tid == 0) *scale_at = s;
 }

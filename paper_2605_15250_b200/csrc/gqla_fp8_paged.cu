@@ -2,6 +2,7 @@
 // and head: argument validation, kernel selection, launch.
 #include "../../include/gqla.h"
 
+#include <algorithm>
 #include <type_traits>
 
 #include "append_rope.cuh"
@@ -74,21 +75,24 @@ void fill(Args& k, const gqla_dims& d, const AppendCall& a) {
 
 int64_t query_blocks(const gqla_dims& d, const AppendCall& a, bool vec, int threads) {
     if (a.q_r == nullptr || d.d_r == 0) return 0;
-    const int64_t items = a.n * d.h_q * (vec ? RopeItem<true>::count(d.d_r) : RopeItem<false>::count(d.d_r));
+    const int64_t items = a.n * d.h_q * (vec ? RopeItem<8>::count(d.d_r) : RopeItem<1>::count(d.d_r));
     return (items + threads - 1) / threads;
 }
 
 template <typename Args>
-gqla_status launch_append(void (*kern)(Args), const Args& a, int64_t blocks, int threads, cudaStream_t st) {
+gqla_status launch_append(void (*kern)(Args), const Args& a, int64_t blocks, int threads, cudaStream_t st, int smem = 0) {
     if (blocks > 0x7fffffffLL) return GQLA_ERR_SHAPE;
-    return tc::launch_pdl(kern, dim3((unsigned)blocks), dim3(threads), 0, st, a) == cudaSuccess ? GQLA_OK : GQLA_ERR_CUDA;
+    if (smem > 48 * 1024 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+        return GQLA_ERR_CUDA;
+    return tc::launch_pdl(kern, dim3((unsigned)blocks), dim3(threads), smem, st, a) == cudaSuccess ? GQLA_OK : GQLA_ERR_CUDA;
 }
 
 template <int THREADS>
 gqla_status launch_append_fp8_of(gqla_dtype dtype, bool vec, const AppendFp8Args& a, int64_t blocks, cudaStream_t st) {
     if (dtype == GQLA_BF16)
-        return launch_append(vec ? append_fp8_kernel<__nv_bfloat16, true, THREADS> : append_fp8_kernel<__nv_bfloat16, false, THREADS>, a,
-                             blocks, THREADS, st);
+        return vec ? launch_append(append_fp8_kernel<__nv_bfloat16, true, THREADS>, a, blocks, THREADS, st,
+                                   a.held * HeldChunks<__nv_bfloat16, true, THREADS>::kBytes)
+                   : launch_append(append_fp8_kernel<__nv_bfloat16, false, THREADS>, a, blocks, THREADS, st);
     return launch_append(vec ? append_fp8_kernel<float, true, THREADS> : append_fp8_kernel<float, false, THREADS>, a, blocks, THREADS, st);
 }
 
@@ -97,12 +101,22 @@ gqla_status launch_append_fp8(const gqla_dims& d, const AppendCall& call, Append
     fill(a, d, call);
     a.block_table = block_table; a.max_pages = max_pages; a.page_size = page_size; a.status = status_word;
     a.n_pages = (int32_t)(n_rows / page_size);
+    for (Fp8Plane& p : a.plane) {
+        const int turned = p.rope_heads ? (vec ? RopeItem<4>::count(d.d_r) : RopeItem<1>::count(d.d_r)) : 0;
+        const int width = p.a_width + (p.rope_heads ? d.d_r : 0), each = vec ? 8 : 1;
+        p.copied = ItemsOfRow(std::max(p.a_width / each, 1));
+        p.turned = ItemsOfRow(std::max(turned, 1));
+        p.coded = ItemsOfRow(std::max(width / each, 1));
+    }
     a.heads_in_all = a.plane[0].heads + a.plane[1].heads + a.plane[2].heads;
     int shift = 0;
     while ((2 << shift) <= page_size) ++shift;
     const int64_t by_pages = (call.n >> shift) + 2 * (int64_t)call.B;
     const int64_t units = call.n < by_pages ? call.n : by_pages;
     a.unit_shift = call.n < by_pages ? -1 : shift;
+    // a unit by rows has a row or a few: room for one chunk a thread leaves that of the next launch's blocks free, which then start
+    // early (64 rows into 17 planes' heads, launches back to back, 128 threads: 7.2 us with room for eight chunks, 5.8 with room for one)
+    a.held = call.n < by_pages ? 1 : 16;
     if (units > 0x7fffffffLL) return GQLA_ERR_SHAPE;
     a.kv_blocks = units * a.heads_in_all;
     const int threads = a.heads_in_all == 1 ? kLatentThreads : kPlaneThreads;
@@ -449,6 +463,7 @@ gqla_status gqla_append_rope(const gqla_dims* d, gqla_dtype dtype, int32_t B, in
     AppendArgs a{};
     fill(a, *d, call);
     a.c = c; a.c_stride = c_row_stride; a.r_kv = d->r_kv;
+    a.items = ItemsOfRow(!vec ? d->r_kv : dtype == GQLA_BF16 ? d->r_kv / 8 : d->r_kv / 4);
     a.cache = cache; a.cache_stride = cache_row_stride; a.cache_rows = cache_rows;
     a.rows = block_table != nullptr ? RowMap{nullptr, block_table, max_pages, page_size} : RowMap{seq_start, nullptr, 0, 1};
     a.status = status_word;

@@ -204,9 +204,12 @@ struct QueryPair {
         uint32_t top = 0;
 #pragma unroll
         for (int c = 0; c < kPer; ++c) top = bf16_max(top, u[c]);
+        float amax = bf16_finite_max(top, [&](auto f) {
 #pragma unroll
-        for (int o = 8; o > 0; o >>= 1) top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, o));
-        const float amax = __uint_as_float(__vmaxu2(top, top >> 16) << 16);
+            for (int c = 0; c < kPer; ++c) f(u[c]);
+        });
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
         const float qs = amax > 0.f ? pow2_scale(amax, -110) : 1.f;
         const float inv = copysignf(__uint_as_float((254u << 23) - __float_as_uint(qs)), sign);  // 1 / qs
 #pragma unroll
