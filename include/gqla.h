@@ -328,9 +328,10 @@ gqla_status gqla_append_planes_fp8(const gqla_dims* dims, gqla_dtype dtype, int3
  *   absorb path  x_t = scale s_t (q_hat . k8_t),                            o = sum_t p_t s_t k8_t[:r_kv] / sum_t p_t
  *   GQA path     x_t = scale (k_s (q_C . k_c8_t) + r_s (q_R . k_r8_t)),     o = sum_t p_t v_s v8_t / sum_t p_t
  * with the scales of token t's page (and the head's group).  Queries come in `dtype` (q_hat [B, s_q, h_q, r_kv+d_r], q
- * [B, s_q, h_q, d_h+d_r]) and are not rounded further than bf16: the tensor-core kernels multiply two E4M3 terms of
+ * [B, s_q, h_q, d_h+d_r]) and are not rounded further than bf16: the tensor-core kernels multiply two eight-bit terms of
  * each query and each probability, which keep as much (a query element below 2^-15 of its row's largest keeps an
- * absolute error of 2^-19 of that one).  Rows of a sequence's last page behind its end may hold anything.
+ * absolute error of 2^-19 of that one; a probability 2^-9 of itself, 2^-8 on the absorb path with s_q * h_q > 64, and
+ * 2^-20 of its row's largest).  Rows of a sequence's last page behind its end may hold anything.
  * Block table, lengths, splits (num_splits >= 1 fixed plan, <= -2 balanced), partials and status word as for
  * gqla_decode_absorb_paged / gqla_decode_gqa_paged; with `out` not NULL ([B, s_q, h_q, r_kv] or [.., d_h] of `dtype`) the call
  * also merges the partials as gqla_combine_splits does (lse fp32 [B, s_q, h_q] or NULL, NULL without out).  Tensor-core kernels:
@@ -349,8 +350,10 @@ gqla_status gqla_decode_gqa_fp8_paged(const gqla_dims* dims, gqla_dtype dtype, i
                                       const float* v_scale, const float* r_scale, const int32_t* block_table,
                                       int32_t max_pages, int32_t page_size, const int32_t* seqlens, float* o_part,
                                       float* lse_part, void* out, float* lse, int32_t* status_word, void* stream);
-/* Workers a balanced call of the two is cut for on the CURRENT device (path: 0 = absorb, 1 = GQA), to be used with
- * gqla_balanced_plan; 0 where the fixed plan is used instead, -1 on error. */
+/* Workers W a balanced call of the two is cut for on the CURRENT device (path: 0 = absorb, 1 = GQA), to choose num_splits
+ * by and to be used with gqla_balanced_plan; 0 where the fixed plan is used instead, -1 on error.  Where there is about a
+ * sequence per worker (W / 2 < B <= W) and the longest is a few tiles of 128 rows longer than a share, every sequence is
+ * one piece in slot 0 instead. */
 int32_t gqla_fp8_paged_workers(const gqla_dims* dims, gqla_dtype dtype, int32_t s_q, int32_t page_size, int32_t path);
 
 /* Log-sum-exp merge of split partials (split-KV is not in the paper; it is the flash-decoding

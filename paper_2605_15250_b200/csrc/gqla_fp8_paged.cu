@@ -253,8 +253,8 @@ bool covers(const gqla_dims& d, gqla_dtype dtype, int32_t s_q, int32_t page_size
            page_size % 16 == 0 && s_q <= 4096;
 }
 
-// Absorb path: CTA pairs with the query rows on M beyond 32 rows.  A pair does 128 rows of a tile in less time than the
-// tokens-on-M kernel's CTAs do 64 of them (64 x 4096 rows, 128 heads: 116 us there), which up to 32 rows is bound by HBM.
+// Absorb path: CTA pairs with the query rows on M beyond 64 rows.  64 sequences of 4096 rows: 64 heads 66 us on the
+// tokens-on-M kernel and 80 on pairs, half of whose rows are empty then; 128 heads 115 and 77.
 bool on_pairs(const gqla_dims& d, int32_t s_q, bool latent) { return latent && (int64_t)s_q * d.h_q > 64; }
 
 // CTA pairs resident at once on the current device, 0 where it cannot be asked.

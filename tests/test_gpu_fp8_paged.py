@@ -298,7 +298,7 @@ def _bounds(p, scale_v, v8, x_err, rounded, terms):
     """Element-wise error bound of softmax(x) V from the kernel's roundings: weights cut to two terms by way of fp16 (2^-12),
     scores off by x_err (twice: numerator and sum), `rounded` of the result for the output's type.  Of a weight in [1, 2) the
     first term, E4M3, leaves at most 2^-4 (half of its spacing 2^-3).  The second one as E4M3 has the spacing 2^-8 there, in
-    [2^-5, 2^-4): it leaves 2^-9.  As E5M2 (`terms`: the absorb path beyond 32 query rows) it has 2^-7 and leaves 2^-8."""
+    [2^-5, 2^-4): it leaves 2^-9.  As E5M2 (`terms`: the absorb path beyond 64 query rows) it has 2^-7 and leaves 2^-8."""
     w = p * scale_v  # [rows, T]
     mag = np.abs(v8)
     rel = w @ mag
@@ -374,7 +374,7 @@ def _check_attention(path, dims, lens, s_q, page, splits, seed=11, gain=1.0, dty
     got, got_lse = _f64(out.t), _f64(lse.t)
     q64 = _f64(q)
     worst = 0.0
-    terms = "e5m2" if path == "absorb" and s_q * h > 32 else "e4m3"
+    terms = "e5m2" if path == "absorb" and s_q * h > 64 else "e4m3"
     for b, T in enumerate(lens):
         at = np.array([int(table[b, t // page]) * page + t % page for t in range(T)], dtype=np.int64)
         pg = at // page
