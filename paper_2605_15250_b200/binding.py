@@ -1,13 +1,13 @@
 """ctypes binding of libgqla.so: one Python function per C entry point, same names.
 
 Argument marshalling only -- every step of the decode path runs in the CUDA
-library.  torch supplies device memory and the current stream.  There is no
+library.  The calls that a serving step makes once per layer with a dozen tensors
+(the appends, the attention over E4M3 pages) are marshalled in C++ (marshal.cpp).  torch supplies device memory and the current stream.  There is no
 fallback: if the library is missing or a call fails, an exception is raised.
 """
 from __future__ import annotations
 
 import ctypes
-import math
 import os
 from ctypes import c_char_p, c_float, c_int32, c_int64, c_void_p
 
@@ -33,6 +33,7 @@ class GqlaError(RuntimeError):
 
 
 _lib = None
+_marshal_module = None
 
 _PROTOTYPES = {
     "gqla_set_policy": (None, [c_int32]),
@@ -453,67 +454,28 @@ def gqla_decode_gqa_fp8(dims: GqlaDims, q8: torch.Tensor, q_scale: torch.Tensor,
 # ------------------------------------------------------------------ appending with rotation, E4M3 pages
 
 
-def _on_current_device(*ts: torch.Tensor | None) -> int:
-    """The calls below are issued on the current device's current stream: their tensors have to live there.  Returns the stream.
-    (These checks run once per call and step: a call of a dozen tensors spent 20 of 25 us in slower forms of them.)"""
-    here = torch.cuda.current_device()
-    for t in ts:
-        if t is not None and t.get_device() != here:
-            raise GqlaError(f"expected a tensor on cuda:{here}, got one on {t.device}")
-    return torch._C._cuda_getCurrentRawStream(here)
+def _marshal():
+    """The module that checks these calls' tensors and makes them (marshal.cpp).  Built along with libgqla.so."""
+    global _marshal_module
+    if _marshal_module is None:
+        try:
+            from . import _marshal as module
+        except ImportError as e:
+            raise GqlaError(f"{e}: build it with `python -m paper_2605_15250_b200.build`") from e
+        if module.built_for.split("+")[0] != torch.__version__.split("+")[0]:
+            raise GqlaError(f"_marshal.so was built for torch {module.built_for}, this is {torch.__version__}: build it again")
+        names = ("gqla_append_rope", "gqla_append_rope_fp8", "gqla_append_planes_fp8", "gqla_decode_absorb_fp8_paged",
+                 "gqla_decode_gqa_fp8_paged", "gqla_status_str")
+        module.bind(GqlaError, *(ctypes.cast(getattr(lib(), name), c_void_p).value for name in names))
+        _marshal_module = module
+    return _marshal_module
 
 
-def _shape(what: str, t: torch.Tensor, shape: tuple, dtype: torch.dtype) -> None:
-    if t.shape != shape or t.dtype is not dtype:
-        raise GqlaError(f"{what}: expected {dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
-
-
-def _dense(what: str, t: torch.Tensor, shape: tuple, dtype: torch.dtype) -> int:
-    """Checks a contiguous tensor; returns its address."""
-    if t.shape != shape or t.dtype is not dtype:
-        raise GqlaError(f"{what}: expected {dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
-    if not t.is_contiguous():
-        raise GqlaError(f"{what}: expected a contiguous tensor")
-    return t.data_ptr()
-
-
-def _rows(what: str, t: torch.Tensor, shape: tuple, dtype: torch.dtype, dim: int = 0) -> int:
-    """Checks a tensor of rows, whose last dimension is contiguous; returns the elements between its rows (steps of `dim`)."""
-    if t.shape != shape or t.dtype is not dtype:
-        raise GqlaError(f"{what}: expected {dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
-    strides = t.stride()
-    if strides[-1] != 1 and shape[-1] > 1:
-        raise GqlaError(f"{what}: the last dimension has to be contiguous")
-    # the stride of a dimension of one element is arbitrary and never stepped by
-    return strides[dim] if shape[dim] > 1 else max(strides[dim], math.prod(shape[dim + 1:]))
-
-
-def _append_args(dims: GqlaDims, n: int, dtype: torch.dtype, k_r, new_start, seqlens, rope, style, q_r, q_out):
-    """(sequences, addresses of new_start and seqlens, arguments from k_r to q_out) that the three append calls share."""
-    B, d_r = seqlens.shape[0], dims.d_r
+def _style(style: str) -> int:
     code = ROPE_STYLES.get(style)
     if code is None:
         raise GqlaError(f"style is one of {sorted(ROPE_STYLES)}, got {style!r}")
-    head = (_dense("new_start", new_start, (B + 1,), torch.int32), _dense("seqlens", seqlens, (B,), torch.int32))
-    mid = [k_r.data_ptr(), _rows("k_r", k_r, (n, d_r), dtype), _dense("rope", rope, (rope.shape[0], d_r), torch.float32),
-           rope.shape[0], code]
-    if (q_r is None) != (q_out is None):
-        raise GqlaError("q_r and q_out come together")
-    if q_r is None:
-        return B, head, (*mid, None, 0, 0, None, 0, 0)
-    shape = (n, dims.h_q, d_r)
-    for name, t in (("q_r", q_r), ("q_out", q_out)):
-        mid += (t.data_ptr(), _rows(name, t, shape, dtype), _rows(name, t, shape, dtype, 1))
-    return B, head, mid
-
-
-def _pages(n_rows: int, block_table: torch.Tensor, page_size: int, B: int) -> int:
-    """Checks a block table and the page size; returns the number of pages."""
-    if block_table.dtype is not torch.int32 or block_table.dim() != 2 or block_table.shape[0] != B or not block_table.is_contiguous():
-        raise GqlaError(f"block_table: expected contiguous int32 [{B}, max_pages], got {block_table.dtype} {tuple(block_table.shape)}")
-    if page_size < 1 or n_rows % page_size != 0:
-        raise GqlaError(f"a cache of {n_rows} rows is not made of pages of {page_size}")
-    return n_rows // page_size
+    return code
 
 
 def gqla_append_rope(dims: GqlaDims, c: torch.Tensor, k_r: torch.Tensor, new_start: torch.Tensor, seqlens: torch.Tensor,
@@ -524,20 +486,8 @@ def gqla_append_rope(dims: GqlaDims, c: torch.Tensor, k_r: torch.Tensor, new_sta
     page_size) and rotates their queries q_r [n, h_q, d_r] into q_out.  c [n, r_kv], k_r [n, d_r]: packed over the
     sequences, sequence b's rows are new_start[b]..new_start[b+1] (int32 [B+1]) and end at position seqlens[b] - 1.
     rope fp32 [positions, d_r] = [cosines ; sines]; style "pairs" (2i, 2i+1) or "halves" (i, i + d_r/2)."""
-    stream = _on_current_device(c, k_r, new_start, seqlens, rope, cache, seq_start, block_table, q_r, q_out, status_word)
-    n, dtype, n_rows = c.shape[0], c.dtype, cache.shape[0]
-    B, head, mid = _append_args(dims, n, dtype, k_r, new_start, seqlens, rope, style, q_r, q_out)
-    c_stride = _rows("c", c, (n, dims.r_kv), dtype)
-    cache_stride = _rows("cache", cache, (n_rows, dims.r_kv + dims.d_r), dtype)
-    if (seq_start is None) == (block_table is None):
-        raise GqlaError("either seq_start (packed) or block_table (paged)")
-    if block_table is not None:
-        _pages(n_rows, block_table, page_size, B)
-        where = (None, block_table.data_ptr(), block_table.shape[1])
-    else:
-        where = (_dense("seq_start", seq_start, (B,), torch.int64), None, 0)
-    _check(lib().gqla_append_rope(ctypes.byref(dims), _dtype_code(c), B, n, *head, c.data_ptr(), c_stride, *mid, cache.data_ptr(),
-                                  cache_stride, n_rows, *where, page_size, _ptr(status_word), stream), "gqla_append_rope")
+    (_marshal_module or _marshal()).gqla_append_rope(dims, c, new_start, seqlens, rope, _style(style), k_r, q_r, q_out, cache, seq_start,
+                                                     block_table, page_size, status_word)
 
 
 def gqla_append_rope_fp8(dims: GqlaDims, c: torch.Tensor, k_r: torch.Tensor, new_start: torch.Tensor, seqlens: torch.Tensor,
@@ -546,25 +496,8 @@ def gqla_append_rope_fp8(dims: GqlaDims, c: torch.Tensor, k_r: torch.Tensor, new
                          status_word: torch.Tensor | None = None) -> None:
     """gqla_append_rope into E4M3 pages: codes cache8 (uint8 [N, r_kv+d_r]) with page_scale fp32 [N / page_size], powers of two
     that grow with the largest value of a page (its older rows are coded anew)."""
-    stream = _on_current_device(c, k_r, new_start, seqlens, rope, cache8, page_scale, block_table, q_r, q_out, status_word)
-    n, dtype, n_rows = c.shape[0], c.dtype, cache8.shape[0]
-    B, head, mid = _append_args(dims, n, dtype, k_r, new_start, seqlens, rope, style, q_r, q_out)
-    c_stride = _rows("c", c, (n, dims.r_kv), dtype)
-    cache_stride = _rows("cache8", cache8, (n_rows, dims.r_kv + dims.d_r), torch.uint8)
-    scale = _dense("page_scale", page_scale, (_pages(n_rows, block_table, page_size, B),), torch.float32)
-    _check(lib().gqla_append_rope_fp8(ctypes.byref(dims), _dtype_code(c), B, n, *head, c.data_ptr(), c_stride, *mid, cache8.data_ptr(),
-                                      cache_stride, n_rows, scale, block_table.data_ptr(), block_table.shape[1], page_size,
-                                      _ptr(status_word), stream), "gqla_append_rope_fp8")
-
-
-def _planes(dims: GqlaDims, k_c8, v8, k_r8, k_scale, v_scale, r_scale, block_table, page_size, B):
-    """Checks the E4M3 planes and their scales; returns (k_c8, v8, k_r8, row stride of k_r8, rows), (k_scale, v_scale, r_scale)."""
-    n_rows, plane = k_c8.shape[0], (k_c8.shape[0], dims.g, dims.d_h)
-    n_pages = _pages(n_rows, block_table, page_size, B)
-    return ((_dense("k_c8", k_c8, plane, torch.uint8), _dense("v8", v8, plane, torch.uint8), k_r8.data_ptr(),
-             _rows("k_r8", k_r8, (n_rows, dims.d_r), torch.uint8), n_rows),
-            (_dense("k_scale", k_scale, (n_pages, dims.g), torch.float32), _dense("v_scale", v_scale, (n_pages, dims.g), torch.float32),
-             _dense("r_scale", r_scale, (n_pages,), torch.float32)))
+    (_marshal_module or _marshal()).gqla_append_rope_fp8(dims, c, new_start, seqlens, rope, _style(style), k_r, q_r, q_out, cache8,
+                                                         page_scale, block_table, page_size, status_word)
 
 
 def gqla_append_planes_fp8(dims: GqlaDims, k_c: torch.Tensor, v: torch.Tensor, k_r: torch.Tensor, new_start: torch.Tensor,
@@ -574,23 +507,8 @@ def gqla_append_planes_fp8(dims: GqlaDims, k_c: torch.Tensor, v: torch.Tensor, k
                            q_out: torch.Tensor | None = None, status_word: torch.Tensor | None = None) -> None:
     """The GQA path's new rows, k_c, v [n, g, d_h] and k_r [n, d_r] (rotated on the way), into E4M3 planes k_c8, v8 [N, g, d_h],
     k_r8 [N, d_r] with a scale per page and group (k_scale, v_scale [N / page_size, g]; r_scale [N / page_size])."""
-    stream = _on_current_device(k_c, v, k_r, new_start, seqlens, rope, k_c8, v8, k_r8, k_scale, v_scale, r_scale, block_table, q_r,
-                                q_out, status_word)
-    n, dtype = k_c.shape[0], k_c.dtype
-    B, head, mid = _append_args(dims, n, dtype, k_r, new_start, seqlens, rope, style, q_r, q_out)
-    new = (_dense("k_c", k_c, (n, dims.g, dims.d_h), dtype), _dense("v", v, (n, dims.g, dims.d_h), dtype))
-    planes, scales = _planes(dims, k_c8, v8, k_r8, k_scale, v_scale, r_scale, block_table, page_size, B)
-    _check(lib().gqla_append_planes_fp8(ctypes.byref(dims), _dtype_code(k_c), B, n, *head, *new, *mid, *planes, *scales,
-                                        block_table.data_ptr(), block_table.shape[1], page_size, _ptr(status_word), stream),
-           "gqla_append_planes_fp8")
-
-
-def _partials(dims: GqlaDims, B: int, s_q: int, num_splits: int, width: int, dtype: torch.dtype, o_part, lse_part, out, lse):
-    """Checks the partials and the merged output; returns their addresses."""
-    h, slots = dims.h_q, abs(num_splits)
-    return (_dense("o_part", o_part, (B, slots, s_q, h, width), torch.float32), _dense("lse_part", lse_part, (B, slots, s_q, h), torch.float32),
-            None if out is None else _dense("out", out, (B, s_q, h, width), dtype),
-            None if lse is None else _dense("lse", lse, (B, s_q, h), torch.float32))
+    (_marshal_module or _marshal()).gqla_append_planes_fp8(dims, k_c, v, new_start, seqlens, rope, _style(style), k_r, q_r, q_out, k_c8, v8,
+                                                           k_r8, k_scale, v_scale, r_scale, block_table, page_size, status_word)
 
 
 def gqla_decode_absorb_fp8_paged(dims: GqlaDims, q_hat: torch.Tensor, cache8: torch.Tensor, page_scale: torch.Tensor,
@@ -599,16 +517,8 @@ def gqla_decode_absorb_fp8_paged(dims: GqlaDims, q_hat: torch.Tensor, cache8: to
                                  lse: torch.Tensor | None = None, status_word: torch.Tensor | None = None) -> None:
     """Absorb-path attention (Eq. (mqa), lines 3-5) over E4M3 pages with a scale per page; q_hat [B,s_q,h_q,r_kv+d_r] in bf16 or
     fp32.  With `out` [B,s_q,h_q,r_kv] the partials are merged by the same call (lse [B,s_q,h_q] optional)."""
-    stream = _on_current_device(q_hat, cache8, page_scale, block_table, seqlens, o_part, lse_part, out, lse, status_word)
-    B, s_q, n_rows, width = q_hat.shape[0], q_hat.shape[1], cache8.shape[0], dims.r_kv + dims.d_r
-    q = _dense("q_hat", q_hat, (B, s_q, dims.h_q, width), q_hat.dtype)
-    cache_stride = _rows("cache8", cache8, (n_rows, width), torch.uint8)
-    page = _dense("page_scale", page_scale, (_pages(n_rows, block_table, page_size, B),), torch.float32)
-    _check(lib().gqla_decode_absorb_fp8_paged(ctypes.byref(dims), _dtype_code(q_hat), B, s_q, scale, num_splits, q, cache8.data_ptr(),
-                                              cache_stride, n_rows, page, block_table.data_ptr(), block_table.shape[1], page_size,
-                                              _dense("seqlens", seqlens, (B,), torch.int32),
-                                              *_partials(dims, B, s_q, num_splits, dims.r_kv, q_hat.dtype, o_part, lse_part, out, lse),
-                                              _ptr(status_word), stream), "gqla_decode_absorb_fp8_paged")
+    (_marshal_module or _marshal()).gqla_decode_absorb_fp8_paged(dims, q_hat, cache8, page_scale, block_table, page_size, seqlens, scale,
+                                                                 num_splits, o_part, lse_part, out, lse, status_word)
 
 
 def gqla_decode_gqa_fp8_paged(dims: GqlaDims, q: torch.Tensor, k_c8: torch.Tensor, v8: torch.Tensor, k_r8: torch.Tensor,
@@ -618,16 +528,8 @@ def gqla_decode_gqa_fp8_paged(dims: GqlaDims, q: torch.Tensor, k_c8: torch.Tenso
                               status_word: torch.Tensor | None = None) -> None:
     """GQA-path attention (Eq. (mha)) over E4M3 planes with a scale per page and group; q [B,s_q,h_q,d_h+d_r] in bf16 or fp32.
     With `out` [B,s_q,h_q,d_h] the partials are merged by the same call (lse [B,s_q,h_q] optional)."""
-    stream = _on_current_device(q, k_c8, v8, k_r8, k_scale, v_scale, r_scale, block_table, seqlens, o_part, lse_part, out, lse,
-                                status_word)
-    B, s_q = q.shape[0], q.shape[1]
-    planes, scales = _planes(dims, k_c8, v8, k_r8, k_scale, v_scale, r_scale, block_table, page_size, B)
-    _check(lib().gqla_decode_gqa_fp8_paged(ctypes.byref(dims), _dtype_code(q), B, s_q, scale, num_splits,
-                                           _dense("q", q, (B, s_q, dims.h_q, dims.d_h + dims.d_r), q.dtype), *planes, *scales,
-                                           block_table.data_ptr(), block_table.shape[1], page_size,
-                                           _dense("seqlens", seqlens, (B,), torch.int32),
-                                           *_partials(dims, B, s_q, num_splits, dims.d_h, q.dtype, o_part, lse_part, out, lse),
-                                           _ptr(status_word), stream), "gqla_decode_gqa_fp8_paged")
+    (_marshal_module or _marshal()).gqla_decode_gqa_fp8_paged(dims, q, k_c8, v8, k_r8, k_scale, v_scale, r_scale, block_table, page_size,
+                                                              seqlens, scale, num_splits, o_part, lse_part, out, lse, status_word)
 
 
 def gqla_fp8_paged_workers(dims: GqlaDims, dtype: torch.dtype, s_q: int, page_size: int, path: str) -> int:

@@ -183,3 +183,19 @@ def test_two_terms_keep_a_bf16_value():
     hi = O.e4m3_decode(O.e4m3_encode(small))
     lo = O.e4m3_decode(O.e4m3_encode(((small - hi) * 16).astype(np.float32))) / 16
     assert (np.abs(hi + lo - small) <= np.maximum(2.0 ** -14, 2.0 ** -9 * small)).all()
+
+
+def test_the_binding_refuses_what_is_not_on_the_gpu():
+    """The argument checks run in the binding's own module, whose messages name the call and the tensor."""
+    d = B.make_dims(128, 8, 128, 512, 64)
+    c = torch.zeros(1, 512, dtype=torch.bfloat16)
+    with pytest.raises(B.GqlaError, match="gqla_append_rope_fp8: c: expected a CUDA tensor"):
+        B.gqla_append_rope_fp8(d, c, None, None, None, None, "pairs", None, None, None, 16)
+    with pytest.raises(B.GqlaError, match="gqla_decode_gqa_fp8_paged: q: expected a tensor, got None"):
+        B.gqla_decode_gqa_fp8_paged(d, None, c, c, c, c, c, c, c, 16, c, 1.0, 1, c, c)
+    with pytest.raises(B.GqlaError, match="q_hat: expected a tensor, got list"):
+        B.gqla_decode_absorb_fp8_paged(d, [1], c, c, c, 16, c, 1.0, 1, c, c)
+    with pytest.raises(B.GqlaError, match="dims"):
+        B.gqla_append_rope(bytearray(8), c, None, None, None, None, "pairs", None, None)
+    with pytest.raises(B.GqlaError, match="style"):
+        B.gqla_append_rope(d, c, None, None, None, None, "half", None, None)
