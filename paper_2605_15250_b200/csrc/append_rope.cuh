@@ -242,7 +242,7 @@ struct AppendArgs {
     int32_t* status;
 };
 
-constexpr int kAppendMostRows = 8;  // new rows of a warp
+constexpr int kAppendMostRows = 4;  // new rows of a warp
 
 // Item i, i + step, i + 2 step, .. of rows of `per` items each, without a division per item.
 struct RowItems {

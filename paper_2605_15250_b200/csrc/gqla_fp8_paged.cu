@@ -467,7 +467,8 @@ gqla_status gqla_append_rope(const gqla_dims* d, gqla_dtype dtype, int32_t B, in
     a.cache = cache; a.cache_stride = cache_row_stride; a.cache_rows = cache_rows;
     a.rows = block_table != nullptr ? RowMap{nullptr, block_table, max_pages, page_size} : RowMap{seq_start, nullptr, 0, 1};
     a.status = status_word;
-    // a row per warp while that does not fill the GPU, eight beyond (each lane then keeps eight loads in flight)
+    // a row per warp while that does not fill the GPU, four beyond (each lane then keeps eight loads of a latent part of 1 KB in
+    // flight; eight rows: 12000 8.3 against 7.8 us, 39000 20.3 against 19.8, 98000 40.9 against 41.3)
     a.per_warp = n_new >= 8192 ? kAppendMostRows : 1;
     const int64_t rows_per_block = (int64_t)a.per_warp * (kAppendThreads / 32);
     const int64_t kv = (n_new + rows_per_block - 1) / rows_per_block;
