@@ -4,8 +4,8 @@
 // takes 128 rows as four CTAs, which read every tile from L2 four times and keep it in shared memory for 32 rows' work;
 // here a pair reads it once (K and V boxes), for 128.
 //
-// Bound by the tensor core and by a piece's ends: a tile's 36 + 16 MMAs of 128 x 128 (x 2 halves of V) take 2540 cycles at E4M3 rate and a
-// tile 2650 to 2800; a piece costs another 18000 (queries 6000, first references 5000, output 7000).  128 heads, 64 x 4096 rows:
+// Bound by the tensor core and by a piece's ends: a tile's MMAs take about 2540 cycles back to back and a tile 2650
+// to 2800 (tensor pipe active 56 % of the SM's cycles); a piece costs another 18000 (queries 6000, first references 5000, output 7000).  128 heads, 64 x 4096 rows:
 // 77 us merge included, 0.95 PFLOP/s of the method's products, each done twice here.
 //
 //   * Queries: hi and lo, both E4M3, written to shared memory by the softmax warps at a piece's start; S = (Q_hi + Q_lo) K^T in one
