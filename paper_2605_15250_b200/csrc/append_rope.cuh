@@ -359,12 +359,6 @@ __device__ __forceinline__ float finite_max(float m, float x) {
     return a <= FLT_MAX && a > m ? a : m;
 }
 
-__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
-    uint32_t r;
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
-
 struct Fp8Plane {
     const void* a;     // first part of a row: width elements, copied
     int64_t a_stride;  // between the rows of the source
@@ -549,7 +543,6 @@ __global__ void __launch_bounds__(THREADS, THREADS == kLatentThreads ? 3 : 16) a
     const float need = pow2_scale(amax, kSmallestScaleExp);
     const float s = need > s_old ? need : s_old;
     const float inv = 1.f / s;
-    const uint32_t inv2 = tc::pack_bf16(inv, inv);
 
     if (lo > p0 && s > s_old) {  // the older rows under the larger scale
         const float ratio = s_old * inv;
@@ -568,11 +561,10 @@ __global__ void __launch_bounds__(THREADS, THREADS == kLatentThreads ? 3 : 16) a
     }
     if constexpr (kHeld > 0) {
         each_held(P.dst_stride, [&](int h, int64_t off) {
-            // times the power of two in bf16: exact but for values below 2^-126, whose codes are zero
-            uint4 u = held[h * THREADS];
-            u = make_uint4(mul_bf16x2(u.x, inv2), mul_bf16x2(u.y, inv2), mul_bf16x2(u.z, inv2), mul_bf16x2(u.w, inv2));
             float v[8];
-            unpack8(u, v);
+            unpack8(held[h * THREADS], v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] *= inv;
             store8(dst + off, v);
         });
     }

@@ -397,7 +397,7 @@ gqla_status decode_fp8_paged(const Fp8PagedCall& c, void* out, float* lse, void*
     gqla_status s = check_dims(d);
     if (s != GQLA_OK) return s;
     if (c.dtype != GQLA_BF16 && c.dtype != GQLA_F32) return GQLA_ERR_DTYPE;
-    if (c.B < 0 || c.s_q < 1 || c.S == 0 || c.S == -1 || c.page_size < 1 || c.max_pages < 1 || c.n_rows < 0 || c.n_rows > 0x7fffffffLL)
+    if (c.B < 0 || c.s_q < 1 || c.S == 0 || c.S == -1 || c.S < -0x7fffffff || c.page_size < 1 || c.max_pages < 1 || c.n_rows < 0 || c.n_rows > 0x7fffffffLL)
         return GQLA_ERR_SHAPE;
     if (c.B == 0) return GQLA_OK;
     const bool rope = !c.latent && d->d_r > 0;

@@ -254,6 +254,24 @@ def test_append_fp8_special_values(rng):
     codes.check("codes")
 
 
+def test_append_keeps_a_larger_scale_of_the_callers(rng):
+    """A page whose older rows came with a scale of another kind: it stays while the new rows fit, and they are coded with it."""
+    page, s_old = 16, 0.3
+    codes = Canaried((page, 576), torch.uint8)
+    codes.t.fill_(0x31)
+    scale = torch.full((1,), s_old, device="cuda")
+    x = rng.standard_normal((3, 512)).astype(np.float32)
+    c = _dev(x, torch.bfloat16)
+    B.gqla_append_rope_fp8(B.make_dims(**LLAMA), c, torch.zeros((3, 64), dtype=torch.bfloat16, device="cuda"), _dev(_starts([3])),
+                           torch.tensor([8], dtype=torch.int32, device="cuda"), _dev(_angles(8, 64)), "pairs", codes.t, scale,
+                           torch.zeros((1, 1), dtype=torch.int32, device="cuda"), page)
+    codes.check("codes")
+    assert float(scale) == float(np.float32(s_old)) and (codes.t[:5] == 0x31).all() and (codes.t[8:] == 0x31).all()
+    got = O.e4m3_decode(codes.t[5:8].cpu().numpy())[:, :512] * float(scale)
+    # half a step of E4M3 (2^-4, or 2^-10 of the scale for the smallest codes), and two roundings of 1 / s and the product before it
+    assert (np.abs(got - _f64(c)) <= np.abs(_f64(c)) * (2.0 ** -4 + 2.0 ** -22) + 2.0 ** -10 * s_old * 1.001).all()
+
+
 @pytest.mark.parametrize("kind", ["bf16", "latent", "planes"])
 def test_append_leaves_out_what_has_no_place(rng, kind):
     """Positions behind the rotation table or the block table and pages outside the cache are left out and reported; the other
@@ -321,7 +339,8 @@ def _attend(q, x, v8, scale_v, limits):
     return o, lse, p
 
 
-def _check_attention(path, dims, lens, s_q, page, splits, seed=11, gain=1.0, dtype=torch.bfloat16, dirty=True, hot=None):
+def _check_attention(path, dims, lens, s_q, page, splits, seed=11, gain=1.0, dtype=torch.bfloat16, dirty=True, hot=None,
+                     scale=None):
     """One call (partials, and merged) over random pages against 64 bits.  dirty: NaN codes in every row that no sequence owns.
     hot: the token whose key is every query's, scaled to take the larger part of the weight."""
     rng = np.random.default_rng(seed)
@@ -352,7 +371,7 @@ def _check_attention(path, dims, lens, s_q, page, splits, seed=11, gain=1.0, dty
     if hot is not None and path == "absorb":
         row = int(table[0, hot // page]) * page + hot % page
         planes[0][0][row, 0] = O.e4m3_encode(np.sign(_f64(q)[0, 0, 0]).astype(np.float32) * 100)
-    scale = 1.0 / math.sqrt(d_h + d_r)
+    scale = 1.0 / math.sqrt(d_h + d_r) if scale is None else scale
     S = abs(splits)
     status = torch.zeros(1, dtype=torch.int32, device="cuda")
     o_part, lse_part = Canaried((Bn, S, s_q, h, dv), torch.float32), Canaried((Bn, S, s_q, h), torch.float32)
@@ -396,8 +415,8 @@ def _check_attention(path, dims, lens, s_q, page, splits, seed=11, gain=1.0, dty
             # sqrt(width) steps), and the elements of q below 2^-15 of the row's largest, off by 2^-19 of it
             x_err = 0.0
             if T:
-                x_err = float(scale * (np.abs(qj) @ np.abs(k).T).max() * (2.0 ** -24 * 4 * math.sqrt(width))
-                              + scale * 2.0 ** -19 * np.abs(qj).max() * np.abs(k).sum(axis=1).max() * 2.0 ** -6)
+                x_err = float(abs(scale) * (np.abs(qj) @ np.abs(k).T).max() * (2.0 ** -24 * 4 * math.sqrt(width))
+                              + abs(scale) * 2.0 ** -19 * np.abs(qj).max() * np.abs(k).sum(axis=1).max() * 2.0 ** -6)
             x_err += 2.0 ** -21 * max(1.0, np.abs(x).max(initial=0.0))
             g_o = got[b, :, j * per:(j + 1) * per].reshape(s_q * per, dv)
             g_l = got_lse[b, :, j * per:(j + 1) * per].reshape(-1)
@@ -461,6 +480,46 @@ def test_attention_flat_and_peaked_scores(path, gain):
 def test_one_key_with_most_of_the_weight(hot):
     _check_attention("absorb", LLAMA, [2000], 1, 64, -2, hot=hot)
     _check_attention("absorb", LLAMA, [2000], 1, 16, 1, hot=hot)
+
+
+@pytest.mark.parametrize("gain", [0.02, 8.0, 40.0])
+@pytest.mark.parametrize("s_q,page", [(1, 64), (2, 16)])
+def test_pairs_flat_and_peaked_scores(gain, s_q, page):
+    _check_attention("absorb", CANON, [1500, 130, 3], s_q, page, -2, gain=gain)
+
+
+@pytest.mark.parametrize("hot", [3, 1999])
+def test_pairs_one_key_with_most_of_the_weight(hot):
+    _check_attention("absorb", CANON, [2000], 1, 64, -2, hot=hot)
+
+
+@pytest.mark.parametrize("path,dims", [("absorb", CANON), ("absorb", LLAMA), ("gqa", LLAMA)])
+@pytest.mark.parametrize("scale", [-0.05, 0.0])
+def test_attention_scale_of_any_sign(path, dims, scale):
+    _check_attention(path, dims, [300, 1, 150], 2, 32, -3, scale=scale)
+
+
+@pytest.mark.parametrize("path,dims", [("absorb", CANON), ("absorb", LLAMA), ("gqa", LLAMA), ("gqa", CANON)])
+@pytest.mark.parametrize("splits", [1, -3])
+def test_attention_over_nothing(path, dims, splits):
+    """Sequences without a token, and of fewer tokens than query positions."""
+    _check_attention(path, dims, [0, 0, 0], 2, 64, splits)
+    _check_attention(path, dims, [1, 0, 2], 4, 16, splits)
+
+
+@pytest.mark.parametrize("path,dims,batch", [("absorb", CANON, 60), ("absorb", LLAMA, 110), ("gqa", LLAMA, 14)])
+@pytest.mark.parametrize("splits", [-2, -5])
+def test_a_piece_per_sequence(rng, path, dims, batch, splits):
+    """About a sequence per worker: each goes to one worker whole, and the slots behind its first are empty."""
+    workers = B.gqla_fp8_paged_workers(B.make_dims(**dims), torch.bfloat16, 1, 64, path)
+    assert workers // 2 < batch <= workers
+    lens = [int(t) for t in rng.integers(300, 640, size=batch)]
+    lens[3], lens[batch // 2], lens[-1] = 0, 1, 0
+    _check_attention(path, dims, lens, 1, 64, splits)
+
+
+def test_one_long_sequence_on_every_pair(rng):
+    _check_attention("absorb", CANON, [9000], 1, 64, -72)
 
 
 def test_large_batch_plan(rng):
