@@ -330,7 +330,7 @@ gqla_status gqla_append_planes_fp8(const gqla_dims* dims, gqla_dtype dtype, int3
  * with the scales of token t's page (and the head's group).  Queries come in `dtype` (q_hat [B, s_q, h_q, r_kv+d_r], q
  * [B, s_q, h_q, d_h+d_r]) and are not rounded further than bf16: the tensor-core kernels multiply two eight-bit terms of
  * each query and each probability, which keep as much (a query element below 2^-15 of its row's largest keeps an
- * absolute error of 2^-19 of that one; a probability 2^-9 of itself, 2^-8 on the absorb path with s_q * h_q > 64, and
+ * absolute error of 2^-19 of that one; a probability 2^-9 of itself, 2^-8 on the absorb path with s_q * h_q > 64 and many pieces, and
  * 2^-20 of its row's largest).  Rows of a sequence's last page behind its end may hold anything.
  * Block table, lengths, splits (num_splits >= 1 fixed plan, <= -2 balanced), partials and status word as for
  * gqla_decode_absorb_paged / gqla_decode_gqa_paged; with `out` not NULL ([B, s_q, h_q, r_kv] or [.., d_h] of `dtype`) the call

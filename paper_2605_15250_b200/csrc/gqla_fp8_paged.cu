@@ -286,11 +286,24 @@ int resident_pairs() {
     return cached[dev];
 }
 
-int32_t workers_of(const gqla_dims& d, int32_t s_q, bool latent) {
-    if (on_pairs(d, s_q, latent)) return resident_pairs() / (int32_t)(((int64_t)s_q * d.h_q + 127) / 128);
+int32_t token_workers(const gqla_dims& d, int32_t s_q, bool latent) {
     const RowBlocks r = row_blocks(s_q, latent ? d.h_q : d.h_q / d.g);
     const int64_t per = r.count() * (latent ? 1 : d.g);
     return per > 0 ? (int32_t)(sm_count() / per) : 0;
+}
+int32_t workers_of(const gqla_dims& d, int32_t s_q, bool latent) {
+    if (on_pairs(d, s_q, latent)) return resident_pairs() / (int32_t)(((int64_t)s_q * d.h_q + 127) / 128);
+    return token_workers(d, s_q, latent);
+}
+
+// Calls of few pieces stay off the pairs: with no more pieces than the tokens-on-M kernel has workers, each has a CTA of its own per 32
+// rows, and twice
+// the SMs of a pair work at its 128 rows.  Absorb path, 128 heads, on pairs and here: one sequence of 777 rows 16.9 and 15.7 us, of 4096 18.4
+// and 15.7; 4 of 1000 18.2 and 16.2; 32 of 128 18.2 and 15.2; in one piece each 32 of 2048 42.6 and 37.9, 32 of 8192 118 and 109.  (The plan is
+// the same for any number of workers that is no less than the pieces: the share is then the longest sequence's, cut into S - 1.)
+bool few_pieces(const Fp8PagedCall& c) {
+    const int64_t pieces = (int64_t)c.B * (c.S < 0 ? -(int64_t)c.S - 1 : c.S);
+    return pieces <= token_workers(*c.d, c.s_q, c.latent);
 }
 
 template <int R, bool LATENT, int PG>
@@ -340,11 +353,11 @@ gqla_status tc_decode_fp8_pairs(const Fp8PagedCall& c, cudaStream_t st) {
 
 template <int PG>
 gqla_status tc_decode_fp8_paged(const Fp8PagedCall& c, cudaStream_t st) {
-    if (on_pairs(*c.d, c.s_q, c.latent)) return tc_decode_fp8_pairs<PG>(c, st);
+    if (on_pairs(*c.d, c.s_q, c.latent) && !few_pieces(c)) return tc_decode_fp8_pairs<PG>(c, st);
     const gqla_dims& d = *c.d;
     const int g = c.latent ? 1 : d.g, heads = d.h_q / g;
     const RowBlocks rb = row_blocks(c.s_q, heads);
-    const int32_t workers = c.S < 0 ? workers_of(d, c.s_q, c.latent) : 0;
+    const int32_t workers = c.S < 0 ? token_workers(d, c.s_q, c.latent) : 0;
     const bool balanced = workers > 0;
     const int32_t S = c.S < 0 ? -c.S : c.S;
     const int64_t units = (balanced ? (int64_t)workers : (int64_t)c.B * S) * g * rb.count();

@@ -23,8 +23,8 @@
 //     outgrew its reference by more than kP8Grow binades.  The producer looks up the scales along with the rows and leaves them in
 //     shared memory.
 //   * R = 16 or 32 query rows per CTA.  More rows (64 heads of the absorb path, s_q > 1) are blocks of 32 on CTAs of their own
-//     that walk the same tiles at the same time, so that the cache comes from HBM once and from L2 otherwise.  (Beyond 64 rows the
-//     absorb path runs on tc_decode_fp8_pair.cuh.)
+//     that walk the same tiles at the same time, so that the cache comes from HBM once and from L2 otherwise.  (Beyond 64 rows
+//     absorb path calls of more pieces than workers here run on tc_decode_fp8_pair.cuh.)
 //   * Measured, merge included.  Absorb path, 32 heads, 128 ragged sequences of up to 16384 rows: 127 us, 4.5 TB/s.  GQA path: 32 heads, 64
 //     of up to 16384, 206 us, 5.5 TB/s, bound by HBM; 128 heads, s_q = 2, 64 of 4096, 131 us, 4.3 TB/s, bound by the softmax warps' issue
 //     slots (32 rows x 128 tokens a tile on one SM) and by what they wait for.

@@ -1,5 +1,5 @@
 // Absorb-path split-KV flash decoding over E4M3 pages with a scale per page (Eq. (mqa), lines 3-5) with the QUERY ROWS on the MMA's M
-// axis, for more than 64 of them: the CTA-pair design of tc_decode_absorb_fp8.cuh (2-CTA cluster, cta_group::2 MMAs of M = 128, each CTA
+// axis, for more than 64 of them and enough pieces: the CTA-pair design of tc_decode_absorb_fp8.cuh (2-CTA cluster, cta_group::2 MMAs of M = 128, each CTA
 // 64 query rows, O in 256 TMEM columns, S in 64) with the precision and the page handling of tc_decode_fp8_paged.cuh.  That kernel
 // takes 128 rows as four CTAs, which read every tile from L2 four times and keep it in shared memory for 32 rows' work;
 // here a pair reads it once (K and V boxes), for 128.

@@ -316,7 +316,7 @@ def _bounds(p, scale_v, v8, x_err, rounded, terms):
     """Element-wise error bound of softmax(x) V from the kernel's roundings: weights cut to two terms by way of fp16 (2^-12),
     scores off by x_err (twice: numerator and sum), `rounded` of the result for the output's type.  Of a weight in [1, 2) the
     first term, E4M3, leaves at most 2^-4 (half of its spacing 2^-3).  The second one as E4M3 has the spacing 2^-8 there, in
-    [2^-5, 2^-4): it leaves 2^-9.  As E5M2 (`terms`: the absorb path beyond 64 query rows) it has 2^-7 and leaves 2^-8."""
+    [2^-5, 2^-4): it leaves 2^-9.  As E5M2 (`terms`: the absorb path beyond 64 query rows and the tokens-on-M kernel's workers) it has 2^-7 and leaves 2^-8."""
     w = p * scale_v  # [rows, T]
     mag = np.abs(v8)
     rel = w @ mag
@@ -393,7 +393,8 @@ def _check_attention(path, dims, lens, s_q, page, splits, seed=11, gain=1.0, dty
     got, got_lse = _f64(out.t), _f64(lse.t)
     q64 = _f64(q)
     worst = 0.0
-    terms = "e5m2" if path == "absorb" and s_q * h > 64 else "e4m3"
+    pieces, sms = Bn * (S if splits > 0 else S - 1), torch.cuda.get_device_properties(0).multi_processor_count
+    terms = "e5m2" if path == "absorb" and s_q * h > 64 and pieces > sms // (s_q * -(-h // 32)) else "e4m3"
     for b, T in enumerate(lens):
         at = np.array([int(table[b, t // page]) * page + t % page for t in range(T)], dtype=np.int64)
         pg = at // page
@@ -441,6 +442,20 @@ def test_attention_over_pages(path, page, splits):
     _check_attention(path, CANON, RAGGED, 2, page, splits)
 
 
+@pytest.mark.parametrize("page", [16, 32, 48, 64, 128, 320])
+@pytest.mark.parametrize("splits", [9, -13])
+def test_pairs_over_pages(page, splits):
+    """More pieces than the tokens-on-M kernel has workers for these rows."""
+    _check_attention("absorb", CANON, RAGGED, 2, page, splits)
+
+
+@pytest.mark.parametrize("dims", [LLAMA, dict(h_q=64, g=8, d_h=128, r_kv=512, d_r=64), dict(h_q=28, g=4, d_h=128, r_kv=512, d_r=64),
+                                  dict(h_q=40, g=1, d_h=128, r_kv=512, d_r=64)])
+def test_pairs_head_layouts(dims):
+    _check_attention("absorb", dims, [300, 5, 1, 257], 3, 64, -20)
+    _check_attention("absorb", dims, [300, 5, 1, 257], 3, 64, 19)
+
+
 @pytest.mark.parametrize("path", ["absorb", "gqa"])
 @pytest.mark.parametrize("dims", [LLAMA, dict(h_q=64, g=8, d_h=128, r_kv=512, d_r=64), dict(h_q=28, g=4, d_h=128, r_kv=512, d_r=64),
                                   dict(h_q=20, g=20, d_h=128, r_kv=512, d_r=64), dict(h_q=40, g=1, d_h=128, r_kv=512, d_r=64),
@@ -486,21 +501,25 @@ def test_one_key_with_most_of_the_weight(hot):
 @pytest.mark.parametrize("s_q,page", [(1, 64), (2, 16)])
 def test_pairs_flat_and_peaked_scores(gain, s_q, page):
     _check_attention("absorb", CANON, [1500, 130, 3], s_q, page, -2, gain=gain)
+    _check_attention("absorb", CANON, [1500, 130, 3], s_q, page, -14, gain=gain)
 
 
 @pytest.mark.parametrize("hot", [3, 1999])
 def test_pairs_one_key_with_most_of_the_weight(hot):
-    _check_attention("absorb", CANON, [2000], 1, 64, -2, hot=hot)
+    _check_attention("absorb", CANON, [2000, 1], 1, 64, -40, hot=hot)
+    _check_attention("absorb", CANON, [2000] + [700] * 39, 1, 64, 1, hot=hot)
 
 
 @pytest.mark.parametrize("path,dims", [("absorb", CANON), ("absorb", LLAMA), ("gqa", LLAMA)])
 @pytest.mark.parametrize("scale", [-0.05, 0.0])
 def test_attention_scale_of_any_sign(path, dims, scale):
     _check_attention(path, dims, [300, 1, 150], 2, 32, -3, scale=scale)
+    if dims is CANON:
+        _check_attention(path, dims, [300, 1, 150], 2, 32, -14, scale=scale)
 
 
 @pytest.mark.parametrize("path,dims", [("absorb", CANON), ("absorb", LLAMA), ("gqa", LLAMA), ("gqa", CANON)])
-@pytest.mark.parametrize("splits", [1, -3])
+@pytest.mark.parametrize("splits", [1, -3, -20, 20])
 def test_attention_over_nothing(path, dims, splits):
     """Sequences without a token, and of fewer tokens than query positions."""
     _check_attention(path, dims, [0, 0, 0], 2, 64, splits)
