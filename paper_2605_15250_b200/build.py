@@ -35,14 +35,16 @@ def build_marshal(force: bool = False) -> str:
     import torch
 
     root = os.path.dirname(torch.__file__)
+    part = f"{MARSHAL_PATH}.{os.getpid()}"  # (a process that has the old one loaded keeps it)
     include = [sysconfig.get_paths()["include"], "/usr/local/cuda/include", os.path.join(root, "include"),
                os.path.join(root, "include", "torch", "csrc", "api", "include")]
-    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-Wall", "-shared", "-fPIC", *(f"-I{d}" for d in include), "-o", MARSHAL_PATH,
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-Wall", "-shared", "-fPIC", *(f"-I{d}" for d in include), "-o", part,
            sources[0], "-L" + os.path.join(root, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python",
            "-Wl,--exclude-libs,libstdc++.a"]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError("g++ failed:\n" + " ".join(cmd) + "\n" + res.stdout + res.stderr)
+    os.replace(part, MARSHAL_PATH)
     return MARSHAL_PATH
 
 
