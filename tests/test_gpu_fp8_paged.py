@@ -17,6 +17,7 @@ pytestmark = pytest.mark.gpu
 CANON = dict(h_q=128, g=8, d_h=128, r_kv=512, d_r=64)
 LLAMA = dict(h_q=32, g=8, d_h=128, r_kv=512, d_r=64)
 TINY = dict(h_q=6, g=2, d_h=10, r_kv=20, d_r=6)
+UNEVEN = dict(h_q=8, g=2, d_h=48, r_kv=96, d_r=16)  # vectors of eight that do not divide a block's threads
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -92,7 +93,7 @@ LENGTHS = {  # lengths and new rows: a step, prompts, both, nothing new, sequenc
 @pytest.mark.parametrize("style", ["pairs", "halves"])
 @pytest.mark.parametrize("case", sorted(LENGTHS))
 @pytest.mark.parametrize("dims,dtype,paged", [(CANON, torch.bfloat16, True), (CANON, torch.float32, False), (TINY, torch.float32, True),
-                                              (TINY, torch.bfloat16, False)])
+                                              (TINY, torch.bfloat16, False), (UNEVEN, torch.bfloat16, True)])
 def test_append_rope_rows_and_queries(rng, dims, dtype, paged, case, style):
     lens, new = LENGTHS[case]
     d, n, page = B.make_dims(**dims), sum(new), 24
@@ -171,7 +172,8 @@ def _same_codes(got, want):
 @pytest.mark.parametrize("style", ["pairs", "halves"])
 @pytest.mark.parametrize("page", [16, 24, 64, 256])
 @pytest.mark.parametrize("case", sorted(LENGTHS))
-@pytest.mark.parametrize("dims,dtype", [(LLAMA, torch.bfloat16), (LLAMA, torch.float32), (TINY, torch.bfloat16), (TINY, torch.float32)])
+@pytest.mark.parametrize("dims,dtype", [(LLAMA, torch.bfloat16), (LLAMA, torch.float32), (TINY, torch.bfloat16), (TINY, torch.float32),
+                                        (UNEVEN, torch.bfloat16)])
 def test_append_fp8_codes_and_scales_bit_for_bit(rng, dims, dtype, case, page, style):
     lens, new = LENGTHS[case]
     d, n = B.make_dims(**dims), sum(new)
