@@ -359,6 +359,8 @@ int32_t gqla_fp8_paged_workers(const gqla_dims* dims, gqla_dtype dtype, int32_t 
 /* Log-sum-exp merge of split partials (split-KV is not in the paper; it is the flash-decoding
  * reduction of the same softmax):  M = max_k lse_k, w_k = exp(lse_k - M),
  *   out = sum_k w_k o_k / sum_k w_k,   lse = M + ln sum_k w_k;  all splits empty -> out = 0, lse = -inf.
+ * A NaN among a row's lse_k makes out and lse of that row NaN; o_part of an empty split (lse_k = -inf) is not looked at
+ * otherwise.
  *   o_part [B, S, rows_per_seq, d_out] fp32, lse_part [B, S, rows_per_seq] fp32 (rows_per_seq = s_q*h_q)
  *   out [B, rows_per_seq, d_out] of out_dtype;  lse [B, rows_per_seq] fp32 or NULL. */
 gqla_status gqla_combine_splits(int32_t B, int32_t rows_per_seq, int32_t num_splits, int32_t d_out,

@@ -103,6 +103,10 @@ __global__ void __launch_bounds__(128) decode_generic_kernel(DecodeArgs a) {
     if (lane == 0 && a.lse_part != nullptr) a.lse_part[row] = l > 0.f ? m + logf(l) : -INFINITY;
 }
 
+// Weight of a slot in a merge, exp(lse - mx), mx the largest lse of the row's slots; 0 where all of them are empty (mx = -inf).  The
+// lse of a piece that holds a NaN is NaN (fmaxf passes it over), and so are its weight, the sum and the merged row.
+__device__ __forceinline__ float slot_weight(float lse, float mx) { return mx > -INFINITY || lse != lse ? expf(lse - mx) : 0.f; }
+
 // Log-sum-exp merge: one block per (b, row).  Weights staged in shared memory.
 template <typename TO>
 __global__ void __launch_bounds__(128) combine_generic_kernel(int32_t B, int32_t rows_per_seq, int32_t S, int32_t d_out,
@@ -122,10 +126,9 @@ __global__ void __launch_bounds__(128) combine_generic_kernel(int32_t B, int32_t
     __syncthreads();
     mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
     __syncthreads();
-    const bool dead = !(mx > -INFINITY);
     float den = 0.f;
     for (int k = threadIdx.x; k < S; k += blockDim.x) {
-        const float wk = dead ? 0.f : expf(lp[(int64_t)k * rows_per_seq] - mx);
+        const float wk = slot_weight(lp[(int64_t)k * rows_per_seq], mx);
         w[k] = wk;
         den += wk;
     }
@@ -133,7 +136,7 @@ __global__ void __launch_bounds__(128) combine_generic_kernel(int32_t B, int32_t
     if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = den;
     __syncthreads();
     den = red[0] + red[1] + red[2] + red[3];
-    const float inv = den > 0.f ? 1.f / den : 0.f;
+    const float inv = den == 0.f ? 0.f : 1.f / den;
     const float* op = o_part + (((int64_t)b * S) * rows_per_seq + rr) * d_out;
     for (int d = threadIdx.x; d < d_out; d += blockDim.x) {
         float acc = 0.f;
@@ -143,7 +146,7 @@ __global__ void __launch_bounds__(128) combine_generic_kernel(int32_t B, int32_t
         }
         stf(out + r * d_out + d, acc * inv);
     }
-    if (lse != nullptr && threadIdx.x == 0) lse[r] = dead ? -INFINITY : mx + logf(den);
+    if (lse != nullptr && threadIdx.x == 0) lse[r] = den == 0.f ? -INFINITY : mx + logf(den);
 }
 
 // Vectorised log-sum-exp merge for d_out % 4 == 0.  A block of 256 threads owns 256 / G items of V output columns each
@@ -218,7 +221,7 @@ __global__ void __launch_bounds__(kCombineThreads, 4) combine_vec_kernel(int64_t
         for (int o = span >> 1; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
         float den = 0.f;
         for (int k = kl; k < S; k += span) {
-            const float e = mx > -INFINITY ? expf(__ldg(lp + (int64_t)k * rows_per_seq) - mx) : 0.f;
+            const float e = slot_weight(__ldg(lp + (int64_t)k * rows_per_seq), mx);
             den += e;
             if (have && k < kc) sw[i * kc + k] = e;
         }
@@ -240,8 +243,7 @@ __global__ void __launch_bounds__(kCombineThreads, 4) combine_vec_kernel(int64_t
                 const int row = i / kc, k = k0 + i % kc;
                 const int64_t bb = (row0 + row) / rows_per_seq;
                 const float mx = smax[row];
-                sw[i] = k < S && mx > -INFINITY
-                            ? expf(__ldg(lse_part + (bb * (S - 1) + k) * rows_per_seq + row0 + row) - mx) : 0.f;
+                sw[i] = k < S ? slot_weight(__ldg(lse_part + (bb * (S - 1) + k) * rows_per_seq + row0 + row), mx) : 0.f;
             }
             __syncthreads();
         }
@@ -288,13 +290,13 @@ __global__ void __launch_bounds__(kCombineThreads, 4) combine_vec_kernel(int64_t
     }
     if (!active) return;
     const float den = sden[rl], mx = smax[rl];
-    const float inv = den > 0.f ? 1.f / den : 0.f;
+    const float inv = den == 0.f ? 0.f : 1.f / den;
 #pragma unroll
     for (int u = 0; u < kF4; ++u) {
         acc[u].x *= inv; acc[u].y *= inv; acc[u].z *= inv; acc[u].w *= inv;
         store4(out + r * d_out + c + 4 * per_row * u, acc[u]);
     }
-    if (lse != nullptr && c == 0) lse[r] = mx > -INFINITY ? mx + logf(den) : -INFINITY;
+    if (lse != nullptr && c == 0) lse[r] = den == 0.f ? -INFINITY : mx + logf(den);
 }
 
 // q_hat[row, r] = sum_d W_UK[j][r][d] * q_c[row, d]  (r < r_kv);  q_hat[row, r_kv + d] = q_r[row, d].
@@ -359,15 +361,14 @@ __global__ void __launch_bounds__(128) combine_up_generic_kernel(int32_t h_q, in
     const float* lp = lse_part + b * S * rows_per_seq + rr;
     float mx = -INFINITY;
     for (int k = 0; k < S; ++k) mx = fmaxf(mx, lp[(int64_t)k * rows_per_seq]);
-    const bool dead = !(mx > -INFINITY);
     float den = 0.f;
-    for (int k = 0; k < S; ++k) den += dead ? 0.f : expf(lp[(int64_t)k * rows_per_seq] - mx);
-    const float inv = den > 0.f ? 1.f / den : 0.f;
+    for (int k = 0; k < S; ++k) den += slot_weight(lp[(int64_t)k * rows_per_seq], mx);
+    const float inv = den == 0.f ? 0.f : 1.f / den;
     const float* op = o_part + (b * S * rows_per_seq + rr) * r_kv;
     for (int r = threadIdx.x; r < r_kv; r += blockDim.x) {
         float acc = 0.f;
         for (int k = 0; k < S; ++k) {
-            const float wk = dead ? 0.f : expf(lp[(int64_t)k * rows_per_seq] - mx);
+            const float wk = slot_weight(lp[(int64_t)k * rows_per_seq], mx);
             if (wk != 0.f) acc = fmaf(wk, op[(int64_t)k * rows_per_seq * r_kv + r], acc);
         }
         os[r] = acc * inv;
@@ -379,7 +380,7 @@ __global__ void __launch_bounds__(128) combine_up_generic_kernel(int32_t h_q, in
         for (int r = 0; r < r_kv; ++r) acc = fmaf(ldf(W + (int64_t)r * d_h + d), os[r], acc);
         stf(o + row * d_h + d, acc);
     }
-    if (lse != nullptr && threadIdx.x == 0) lse[row] = dead ? -INFINITY : mx + logf(den);
+    if (lse != nullptr && threadIdx.x == 0) lse[row] = den == 0.f ? -INFINITY : mx + logf(den);
 }
 
 // K_C[n, j, d] = sum_r W_UK[j][r][d] c[n][r],  V likewise with W_UV,  k_R[n] = cache[n, r_kv:].

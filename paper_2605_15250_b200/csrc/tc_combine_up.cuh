@@ -170,17 +170,17 @@ combine_up_tc_kernel(const CombineUpParams p, const __grid_constant__ CUtensorMa
                 for (int o = 4; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
 #pragma unroll
                 for (int i = 0; i < L::kMaxS / 8; ++i) {
-                    v[i] = M > -INFINITY ? expf(v[i] - M) : 0.f;
+                    v[i] = M > -INFINITY || v[i] != v[i] ? expf(v[i] - M) : 0.f;  // (a NaN lse, passed over by fmaxf, makes the row NaN)
                     den += v[i];
                 }
 #pragma unroll
                 for (int o = 4; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
-                const float inv = den > 0.f ? 1.f / den : 0.f;
+                const float inv = den == 0.f ? 0.f : 1.f / den;
                 __syncwarp();  // the previous tile's weights have been read
 #pragma unroll
                 for (int i = 0; i < L::kMaxS / 8; ++i)
                     if (k0 + 8 * i < p.S) w_warp[(lane >> 3) * L::kMaxS + k0 + 8 * i] = inv == 0.f ? 0.f : v[i] * inv;
-                if (have && k0 == 0 && p.lse != nullptr) p.lse[orow] = den > 0.f ? M + logf(den) : -INFINITY;
+                if (have && k0 == 0 && p.lse != nullptr) p.lse[orow] = den == 0.f ? -INFINITY : M + logf(den);
             }
             __syncwarp();
 #pragma unroll 1
