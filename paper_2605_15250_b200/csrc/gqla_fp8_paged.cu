@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(128) decode_fp8_paged_generic_kernel(const Fp8
         const float x = warp_sum(fmaf(dA, sA, dB * sB)) * a.scale;
         const float m_new = fmaxf(m, x);
         const float corr = m > -INFINITY ? expf(m - m_new) : 0.f;
-        const float e = m_new > -INFINITY ? expf(x - m_new) : 0.f;
+        const float e = m_new > -INFINITY || x != x ? expf(x - m_new) : 0.f;  // (fmaxf passes a NaN over: it makes the sum NaN)
         l = l * corr + e;
         const float w = e * sV;
         const e4m3* vr = a.v + n * a.v_stride + (int64_t)j * a.dv;
@@ -217,13 +217,13 @@ __global__ void __launch_bounds__(128) decode_fp8_paged_generic_kernel(const Fp8
         }
         m = m_new;
     }
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const float inv = l == 0.f ? 0.f : 1.f / l;  // (nothing visible)
 #pragma unroll
     for (int c = 0; c < kGenericCols; ++c) {
         const int d = lane + 32 * c;
         if (d < a.dv) a.o_part[row * a.dv + d] = acc[c] * inv;
     }
-    if (lane == 0) a.lse_part[row] = l > 0.f ? m + logf(l) : -INFINITY;
+    if (lane == 0) a.lse_part[row] = l == 0.f ? -INFINITY : m + logf(l);
 }
 
 int pow2_at_least(int x) {

@@ -712,9 +712,9 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
                 const int r = r0 + lane % 8, pq = pq0 + (r >> p.hshift), il = i0 + (r & hmask);
                 const float4 s4 = *reinterpret_cast<const float4*>(sums + 4 * r);
                 const float Lt = ok && pc.n_tiles > 0 ? (s4.x + s4.y) + (s4.z + s4.w) : 0.f;
-                f = Lt > 0.f ? 1.f / Lt : 0.f;
+                f = Lt == 0.f ? 0.f : 1.f / Lt;  // zero: the row sees nothing (its largest weight is at least 2^6 otherwise, or NaN)
                 if (q == 0 && lane < 8 && il < p.hpg && pq < p.s_q)
-                    p.lse_part[out_row0 + (int64_t)pq * p.h_q + il] = Lt > 0.f ? (refs[r] + log2f(Lt)) * 0.6931471805599453f : -INFINITY;
+                    p.lse_part[out_row0 + (int64_t)pq * p.h_q + il] = Lt == 0.f ? -INFINITY : (refs[r] + log2f(Lt)) * 0.6931471805599453f;
             }
 #pragma unroll 1
             for (int m = 0; m < KB; ++m) {
@@ -729,7 +729,7 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
 #pragma unroll
                     for (int c = 0; c < 8; ++c) {
                         const float w = __shfl_sync(0xffffffffu, f, c);
-                        if (w > 0.f) acc[c] = fmaf(__uint_as_float(o[1][c]), 1.f / kP8Lo, __uint_as_float(o[0][c])) * w;
+                        if (w != 0.f) acc[c] = fmaf(__uint_as_float(o[1][c]), 1.f / kP8Lo, __uint_as_float(o[0][c])) * w;
                     }
                 }
 #pragma unroll

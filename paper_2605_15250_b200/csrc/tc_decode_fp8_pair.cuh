@@ -582,7 +582,7 @@ decode_fp8_pair_kernel(const Fp8PairParams p, const __grid_constant__ CUtensorMa
             if (lane == 0) mbar_arrive(fin);
             if (!__all_sync(0xffffffffu, mbar_wait(fin, pi & 1, ab, 11))) ok = false;
             const float Lt = (sm_l[r] + sm_l[64 + r]) + (sm_l[128 + r] + sm_l[192 + r]);
-            const bool live = ok && n_tiles > 0 && Lt > 0.f && m_used > -INFINITY;
+            const bool live = ok && n_tiles > 0 && Lt != 0.f;  // the row sees something (a NaN sum is something)
             const float inv = live ? 1.f / Lt : 0.f;
             // The output rows leave through shared memory (P and the V ring are idle now: the last P.V has completed): every warp turns 32
             // rows x 64 columns of MMA m's block by itself and stores two rows of 256 bytes at a time.  (As bulk stores of 256 bytes, of

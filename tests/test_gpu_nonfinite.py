@@ -93,3 +93,134 @@ def test_merge_with_up_projection_passes_on_a_nan(dims, dtype, slots):
     bound = eps * (up(o_hat.abs(), w_uv.double().abs()) * (1 + eps) + want.abs())
     _same(o, want, bound[~want.isnan()])
     assert torch.equal(lse.isneginf(), want_lse.isneginf()) and torch.equal(lse.isnan(), want_lse.isnan())
+
+
+# ------------------------------------------------------------------ attention over E4M3 pages
+
+LENS, PAGE, S_Q = [300, 130, 65, 0, 1], 32, 2
+# kernel: dimensions, path, splits that lead to it, policy, type of the queries
+KERNELS = {
+    "absorb": ((32, 8, 128, 512, 64), "absorb", (-3, 3, 1), B.POLICY_AUTO, torch.bfloat16),
+    "pairs": ((128, 8, 128, 512, 64), "absorb", (-14, 9), B.POLICY_AUTO, torch.bfloat16),
+    "gqa": ((32, 8, 128, 512, 64), "gqa", (-3, 3, 1), B.POLICY_AUTO, torch.bfloat16),
+    "generic_absorb": ((32, 8, 128, 512, 64), "absorb", (-3, 1), B.POLICY_GENERIC, torch.bfloat16),
+    "generic_gqa": ((6, 2, 10, 20, 6), "gqa", (3,), B.POLICY_AUTO, torch.float32),
+}
+RUNS = [(k, s) for k in KERNELS for s in KERNELS[k][2]]
+
+
+class Attention:
+    """A small call over random finite pages; `run` gives (out, lse) of what its tensors hold then."""
+
+    def __init__(self, kernel, splits, seed=5):
+        (self.h, self.g, d_h, r_kv, d_r), self.path, _, self.policy, dtype = KERNELS[kernel]
+        self.d, self.splits = B.make_dims(self.h, self.g, d_h, r_kv, d_r), splits
+        gen = torch.Generator().manual_seed(seed)
+        counts = [-(-t // PAGE) for t in LENS]
+        n_pages = sum(counts) + 2
+        order = torch.randperm(n_pages, generator=gen).tolist()
+        self.table = torch.zeros((len(LENS), max(counts)), dtype=torch.int32)
+        for i, c in enumerate(counts):
+            self.table[i, :c] = torch.tensor([order.pop() for _ in range(c)], dtype=torch.int32)
+
+        def plane(heads, width):
+            codes = torch.randint(0, 0x78, (n_pages * PAGE, heads, width), generator=gen, dtype=torch.uint8)
+            codes |= torch.randint(0, 2, codes.shape, generator=gen, dtype=torch.uint8) << 7
+            return codes.cuda(), torch.exp2(torch.randint(-9, -5, (n_pages, heads), generator=gen).float()).cuda()
+
+        self.q_split, width, self.dv = (r_kv, r_kv + d_r, r_kv) if self.path == "absorb" else (d_h, d_h + d_r, d_h)
+        self.planes = [plane(1, width)] if self.path == "absorb" else [plane(self.g, d_h), plane(self.g, d_h), plane(1, d_r)]
+        self.q = (torch.randn((len(LENS), S_Q, self.h, width), generator=gen) * 0.1).to(dtype).cuda()
+        self.table, self.lens = self.table.cuda(), torch.tensor(LENS, dtype=torch.int32).cuda()
+
+    def row(self, b, t):
+        return int(self.table[b, t // PAGE]) * PAGE + t % PAGE
+
+    def run(self):
+        slots, shape = abs(self.splits), (len(LENS), S_Q, self.h)
+        o_part = torch.full((shape[0], slots, *shape[1:], self.dv), 5.0, device="cuda")
+        lse_part = torch.full((shape[0], slots, *shape[1:]), 5.0, device="cuda")
+        out, lse = torch.full((*shape, self.dv), 5.0, dtype=self.q.dtype, device="cuda"), torch.full(shape, 5.0, device="cuda")
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        tail = (self.table, PAGE, self.lens, 0.08, self.splits, o_part, lse_part, out, lse, status)
+        p = self.planes
+        B.set_policy(self.policy)
+        try:
+            if self.path == "absorb":
+                B.gqla_decode_absorb_fp8_paged(self.d, self.q, p[0][0][:, 0], p[0][1][:, 0], *tail)
+            else:
+                B.gqla_decode_gqa_fp8_paged(self.d, self.q, p[0][0], p[1][0], p[2][0][:, 0], p[0][1], p[1][1], p[2][1][:, 0], *tail)
+        finally:
+            B.set_policy(B.POLICY_AUTO)
+        assert int(status) == 0
+        return out, lse
+
+
+def _only(got, clean, rows):
+    """out and lse of `rows` (a mask) are NaN, all others what they were."""
+    for x, c in zip(got, clean):
+        assert bool(x[rows].isnan().all())
+        assert torch.equal(x[~rows], c[~rows])
+
+
+@pytest.mark.parametrize("kernel,splits", RUNS)
+@pytest.mark.parametrize("b,t", [(0, 0), (0, 200), (0, 298), (1, 127), (4, 0)])
+def test_a_nan_key_makes_its_rows_nan(kernel, splits, b, t):
+    """A NaN code in a row that both positions of the step see (the last sequence: its one row is seen by the last position)."""
+    a = Attention(kernel, splits)
+    clean = a.run()
+    assert all(not bool(x.isnan().any()) for x in clean)
+    for plane in (0,) if a.path == "absorb" else (0, 2):
+        codes = a.planes[plane][0]
+        head = codes.shape[1] // 2
+        before = codes[a.row(b, t)].clone()
+        codes[a.row(b, t), head, -1] = 0x7F
+        rows = torch.zeros((len(LENS), S_Q, a.h), dtype=torch.bool, device="cuda")
+        of = a.h // codes.shape[1]
+        rows[b, 1 if b == 4 else 0:, head * of:(head + 1) * of] = True
+        got = a.run()
+        if b == 4 and kernel != "generic_absorb" and a.path == "absorb":
+            # (a value NaN times a hidden weight of zero: only lse of the position that does not see the row is kept)
+            assert torch.equal(got[1][4, 0], clean[1][4, 0]) and bool(got[0][4, 1].isnan().all()) and bool(got[1][4, 1].isnan().all())
+            assert torch.equal(got[0][:4], clean[0][:4]) and torch.equal(got[1][:4], clean[1][:4])
+        else:
+            _only(got, clean, rows)
+        codes[a.row(b, t)] = before
+
+
+@pytest.mark.parametrize("kernel,splits", [r for r in RUNS if "gqa" in r[0]])
+def test_a_nan_value_makes_its_column_nan(kernel, splits):
+    a = Attention(kernel, splits)
+    out, lse = a.run()
+    a.planes[1][0][a.row(0, 150), 1, 3] = 0xFF
+    got, got_lse = a.run()
+    of = a.h // a.g
+    assert torch.equal(got_lse, lse) and bool(got[0, :, of:2 * of, 3].isnan().all())
+    got[0, :, of:2 * of, 3] = out[0, :, of:2 * of, 3]
+    assert torch.equal(got, out)
+
+
+@pytest.mark.parametrize("kernel,splits", RUNS)
+def test_a_nan_in_the_last_row_and_the_position_before(kernel, splits):
+    """The step's first position does not see its last row: no NaN reaches lse there, nor any other column of out than the NaN's."""
+    a = Attention(kernel, splits)
+    out, lse = a.run()
+    col = 3
+    plane = a.planes[0 if a.path == "absorb" else 1][0]
+    plane[a.row(0, LENS[0] - 1), :, col] = 0x7F
+    got, got_lse = a.run()
+    assert torch.equal(got_lse[:, 0], lse[:, 0]) and torch.equal(got_lse[1:], lse[1:]) and torch.equal(got[1:], out[1:])
+    others = torch.arange(a.dv, device="cuda") != col
+    assert torch.equal(got[0, 0, :, others], out[0, 0, :, others]) and bool(got[0, 1, :, col].isnan().all())
+    assert a.path == "gqa" or bool(got_lse[0, 1].isnan().all())
+
+
+@pytest.mark.parametrize("kernel,splits", RUNS)
+def test_a_nan_query_makes_its_row_nan(kernel, splits):
+    a = Attention(kernel, splits)
+    clean = a.run()
+    rows = torch.zeros((len(LENS), S_Q, a.h), dtype=torch.bool, device="cuda")
+    for b, p, head, col in ((0, 0, 0, 0), (0, 1, a.h - 1, -1), (1, 0, a.h // 2, a.q_split), (4, 1, 1, 5), (3, 0, 2, 2), (4, 0, 2, 2)):
+        a.q[b, p, head, col] = math.nan
+        rows[b, p, head] = b != 3 and (b, p) != (4, 0)  # (those see nothing: zeros and -inf)
+    _only(a.run(), clean, rows)
