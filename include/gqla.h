@@ -332,7 +332,7 @@ gqla_status gqla_append_planes_fp8(const gqla_dims* dims, gqla_dtype dtype, int3
  * each query and each probability, which keep as much (a query element below 2^-15 of its row's largest keeps an
  * absolute error of 2^-19 of that one; a probability 2^-9 of itself, 2^-8 on the absorb path with s_q * h_q > 64 and many pieces, and
  * 2^-20 of its row's largest).  Rows of a sequence's last page behind its end may hold anything.
- * NaN: a query row that holds one, or that sees a key row with a NaN code (absorb path: anywhere in the row; GQA path: K_C of
+ * NaN: a query row that holds one or an infinity, or that sees a key row with a NaN code (absorb path: anywhere in the row; GQA path: K_C of
  * its group or k_R), gets out and lse NaN, also through the merges; a NaN code in V makes its column of out NaN.  What a row
  * does not see leaves its lse alone; on the tensor-core kernels a NaN in the values of one of the step's own rows may reach
  * the same column of out at the step's earlier positions.

@@ -34,7 +34,7 @@
 //   * The softmax warps read the query rows, cut them and write the swizzled operand themselves, at a piece's start.
 //   * Issuers and producer run converged (tc_common.cuh).
 #pragma once
-#include "append_rope.cuh"  // pow2_scale, finite_max
+#include "append_rope.cuh"  // pow2_scale, bf16_max
 #include "common.cuh"
 #include "sched.cuh"
 #include "tc_common.cuh"
@@ -202,16 +202,15 @@ struct QueryPair {
             u[c] = valid && ci < kChunks ? reinterpret_cast<const uint4*>(row)[ci] : make_uint4(0, 0, 0, 0);
         }
     }
-    // Hands column 8 ci .. + 7's codes to store(first column, hi, lo); returns the row's scale.  sign: of the stored values.
+    // Hands column 8 ci .. + 7's codes to store(first column, hi, lo); returns the row's scale, NaN for a row with an infinity.  sign: of
+    // the stored values.
     template <typename F>
     __device__ __forceinline__ float cut(int lane, float sign, F store) const {
         uint32_t top = 0;
 #pragma unroll
         for (int c = 0; c < kPer; ++c) top = bf16_max(top, u[c]);
-        float amax = bf16_finite_max(top, [&](auto f) {
-#pragma unroll
-            for (int c = 0; c < kPer; ++c) f(u[c]);
-        });
+        top &= 0x7fff7fffu;
+        float amax = __uint_as_float(max(top & 0xffffu, top >> 16) << 16);
 #pragma unroll
         for (int o = 8; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
         const float qs = amax > 0.f ? pow2_scale(amax, -110) : 1.f;
@@ -223,7 +222,8 @@ struct QueryPair {
             split_query8(u[c], inv, hi, lo);
             if (ci < kChunks) store(ci * 8, hi, lo);
         }
-        return qs;
+        // codes have no infinity: the scale makes a row's scores NaN (NaN elements, which amax may miss, are NaN codes)
+        return amax <= FLT_MAX ? qs : __uint_as_float(0x7fffffffu);
     }
 };
 // OR of a predicate over the `nthreads` threads that call it on named barrier `id`.  (Warps that meet in barriers leave a loop by

@@ -17,7 +17,7 @@
 //     with the rows and passed through shared memory behind a barrier of their own (the tile's full barriers are the leader CTA's).
 //   * Shared memory: two terms of Q 72 KB, of P 16 KB, K in a ring of three half tiles, V in one of four.
 #pragma once
-#include "append_rope.cuh"  // pow2_scale, finite_max
+#include "append_rope.cuh"  // pow2_scale
 #include "common.cuh"
 #include "sched.cuh"
 #include "tc_common.cuh"

@@ -136,13 +136,13 @@ class Attention:
     def row(self, b, t):
         return int(self.table[b, t // PAGE]) * PAGE + t % PAGE
 
-    def run(self):
+    def run(self, scale=0.08):
         slots, shape = abs(self.splits), (len(LENS), S_Q, self.h)
         o_part = torch.full((shape[0], slots, *shape[1:], self.dv), 5.0, device="cuda")
         lse_part = torch.full((shape[0], slots, *shape[1:]), 5.0, device="cuda")
         out, lse = torch.full((*shape, self.dv), 5.0, dtype=self.q.dtype, device="cuda"), torch.full(shape, 5.0, device="cuda")
         status = torch.zeros(1, dtype=torch.int32, device="cuda")
-        tail = (self.table, PAGE, self.lens, 0.08, self.splits, o_part, lse_part, out, lse, status)
+        tail = (self.table, PAGE, self.lens, scale, self.splits, o_part, lse_part, out, lse, status)
         p = self.planes
         B.set_policy(self.policy)
         try:
@@ -224,3 +224,27 @@ def test_a_nan_query_makes_its_row_nan(kernel, splits):
         a.q[b, p, head, col] = math.nan
         rows[b, p, head] = b != 3 and (b, p) != (4, 0)  # (those see nothing: zeros and -inf)
     _only(a.run(), clean, rows)
+
+
+@pytest.mark.parametrize("value", [math.inf, -math.inf])
+@pytest.mark.parametrize("kernel,splits", RUNS)
+def test_an_infinite_query_makes_its_row_nan(kernel, splits, value):
+    """Whatever the signs of the keys: alone among small elements, among large ones, twice in a row."""
+    a = Attention(kernel, splits)
+    clean = a.run()
+    rows = torch.zeros((len(LENS), S_Q, a.h), dtype=torch.bool, device="cuda")
+    for b, p, head, col in ((0, 0, 0, 0), (0, 1, a.h - 1, -1), (0, 1, a.h - 1, 4), (1, 0, a.h // 2, a.q_split), (2, 1, 3, 7), (4, 1, 1, 5),
+                            (3, 0, 2, 2), (4, 0, 2, 2)):
+        a.q[b, p, head, col] = value
+        rows[b, p, head] = b != 3 and (b, p) != (4, 0)
+    _only(a.run(), clean, rows)
+
+
+@pytest.mark.parametrize("kernel,splits", [r for r in RUNS if "generic" not in r[0]])
+def test_huge_queries_are_no_infinities(kernel, splits):
+    """Rows times a power of two, which the softmax scale takes away again: bit for bit the same."""
+    a = Attention(kernel, splits)
+    out, lse = a.run()
+    a.q = a.q * 2.0 ** 118
+    big, big_lse = a.run(0.08 * 2.0 ** -118)
+    assert torch.equal(big, out) and torch.equal(big_lse, lse)
