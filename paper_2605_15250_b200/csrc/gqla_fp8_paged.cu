@@ -110,7 +110,7 @@ gqla_status launch_append_fp8(const gqla_dims& d, const AppendCall& call, Append
     }
     a.heads_in_all = a.plane[0].heads + a.plane[1].heads + a.plane[2].heads;
     int shift = 0;
-    while ((2 << shift) <= page_size) ++shift;
+    while (((int64_t)2 << shift) <= page_size) ++shift;  // 2^shift <= page_size < 2^(shift + 1)
     const int64_t by_pages = (call.n >> shift) + 2 * (int64_t)call.B;
     const int64_t units = call.n < by_pages ? call.n : by_pages;
     a.unit_shift = call.n < by_pages ? -1 : shift;
