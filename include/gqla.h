@@ -356,8 +356,8 @@ gqla_status gqla_decode_gqa_fp8_paged(const gqla_dims* dims, gqla_dtype dtype, i
                                       float* lse_part, void* out, float* lse, int32_t* status_word, void* stream);
 /* Workers W a balanced call of the two is cut for on the CURRENT device (path: 0 = absorb, 1 = GQA), to choose num_splits
  * by and to be used with gqla_balanced_plan; 0 where the fixed plan is used instead, -1 on error.  Where there is about a
- * sequence per worker (W / 2 < B <= W) and the longest is a few tiles of 128 rows longer than a share, every sequence is
- * one piece in slot 0 instead. */
+ * sequence per worker (B <= W < 2 B), a share is more than one tile of 128 rows and the longest sequence at most 6 tiles (3 on
+ * the absorb path with s_q * h_q <= 64) longer than it, every sequence is one piece in slot 0 instead. */
 int32_t gqla_fp8_paged_workers(const gqla_dims* dims, gqla_dtype dtype, int32_t s_q, int32_t page_size, int32_t path);
 
 /* Log-sum-exp merge of split partials (split-KV is not in the paper; it is the flash-decoding

@@ -300,14 +300,17 @@ int32_t workers_of(const gqla_dims& d, int32_t s_q, bool latent) {
 }
 
 // Calls of few pieces stay off the pairs: with no more pieces than the tokens-on-M kernel has workers, each has a CTA of its own per 32
-// rows, and twice
-// the SMs of a pair work at its 128 rows.  Absorb path, 128 heads, on pairs and here: one sequence of 777 rows 16.9 and 15.7 us, of 4096 18.4
-// and 15.7; 4 of 1000 18.2 and 16.2; 32 of 128 18.2 and 15.2; in one piece each 32 of 2048 42.6 and 37.9, 32 of 8192 118 and 109.  (The plan is
-// the same for any number of workers that is no less than the pieces: the share is then the longest sequence's, cut into S - 1.)
+// rows, and twice the SMs of a pair work at its 128 rows.  Absorb path, 128 heads, on pairs and here: one sequence of 777 rows 16.9 and
+// 15.7 us, of 4096 18.4 and 15.7; 4 of 1000 18.2 and 16.2; 32 of 128 18.2 and 15.2; in one piece each 32 of 2048 42.6 and 37.9, 32 of 8192
+// 118 and 109.  (The cut is the same for any number of workers that is no less than the pieces: the share is then the longest sequence's,
+// cut into S - 1.  Whether to cut at all goes by workers_of, which the caller knows: WholeOrBalanced.)
 bool few_pieces(const Fp8PagedCall& c) {
     const int64_t pieces = (int64_t)c.B * (c.S < 0 ? -(int64_t)c.S - 1 : c.S);
-    return pieces <= token_workers(*c.d, c.s_q, c.latent);
+    return pieces <= std::min(token_workers(*c.d, c.s_q, c.latent), c.S < 0 ? workers_of(*c.d, c.s_q, c.latent) : 0x7fffffff);
 }
+
+// Tiles by which the longest sequence may exceed a share for every sequence to be one piece.
+int32_t whole_slack(const gqla_dims& d, int32_t s_q, bool latent) { return latent && !on_pairs(d, s_q, latent) ? 3 : 6; }
 
 template <int R, bool LATENT, int PG>
 cudaError_t launch_tc(const tc::Fp8PagedParams& p, const CUtensorMap& k, const CUtensorMap& r, const CUtensorMap& v,
@@ -340,7 +343,7 @@ gqla_status tc_decode_fp8_pairs(const Fp8PagedCall& c, cudaStream_t st) {
         return GQLA_ERR_CUDA;
     tc::Fp8PairParams p{};
     p.B = c.B; p.S = S; p.s_q = c.s_q; p.h_q = d.h_q; p.rows_total = (int32_t)rows_total; p.row_blocks = (int32_t)row_blocks;
-    p.balanced = balanced ? 1 : 0; p.W = workers;
+    p.balanced = balanced ? 1 : 0; p.W = workers; p.slack = whole_slack(d, c.s_q, true);
     p.n_rows = (int32_t)c.n_rows; p.n_pages = (int32_t)(c.n_rows / c.page_size);
     p.scale_log2 = c.scale * 1.4426950408889634f;
     p.q = (const __nv_bfloat16*)c.q; p.page_scale = c.k_scale;
@@ -360,7 +363,8 @@ gqla_status tc_decode_fp8_paged(const Fp8PagedCall& c, cudaStream_t st) {
     const gqla_dims& d = *c.d;
     const int g = c.latent ? 1 : d.g, heads = d.h_q / g;
     const RowBlocks rb = row_blocks(c.s_q, heads);
-    const int32_t workers = c.S < 0 ? token_workers(d, c.s_q, c.latent) : 0;
+    const int32_t plan_workers = c.S < 0 ? workers_of(d, c.s_q, c.latent) : 0;
+    const int32_t workers = plan_workers > 0 ? token_workers(d, c.s_q, c.latent) : 0;
     const bool balanced = workers > 0;
     const int32_t S = c.S < 0 ? -c.S : c.S;
     const int64_t units = (balanced ? (int64_t)workers : (int64_t)c.B * S) * g * rb.count();
@@ -389,7 +393,7 @@ gqla_status tc_decode_fp8_paged(const Fp8PagedCall& c, cudaStream_t st) {
     p.B = c.B; p.S = S; p.s_q = c.s_q; p.h_q = d.h_q; p.g = g; p.hpg = heads;
     p.hb = rb.hb; p.n_hb = rb.n_hb; p.row_blocks = (int32_t)rb.count();
     while ((1 << p.hshift) < rb.hb) ++p.hshift;
-    p.balanced = balanced ? 1 : 0; p.W = workers;
+    p.balanced = balanced ? 1 : 0; p.W = workers; p.plan_W = plan_workers; p.slack = whole_slack(d, c.s_q, c.latent);
     p.n_rows = (int32_t)c.n_rows; p.n_pages = (int32_t)(c.n_rows / c.page_size);
     p.scale_log2 = c.scale * 1.4426950408889634f;
     p.q = (const __nv_bfloat16*)c.q;

@@ -272,19 +272,21 @@ __device__ inline BalancedStart balanced_prepass(const int32_t* seqlens, int32_t
 // where there is about a sequence per worker and the longest is hardly longer than a share.  Cutting 64 sequences of 32 tiles into
 // 74 shares of 28 saves four tiles and costs nearly every worker a second piece, i.e. a second set of queries, first references and
 // outputs (absorb path, 128 heads, merge included: 83 us cut, 77 whole).  `slack`: tiles that a piece's start and end are worth.  Shares of
-// one tile are one piece each, so there the balanced plan has nothing to save.
+// one tile are one piece each, so there the balanced plan has nothing to save.  `plan_W`: the workers that the caller was told of, by whom
+// the choice goes; W: those of this grid.  They differ only where there are no more pieces than either, B (S - 1) <= W <= plan_W; the
+// share is then the longest sequence's tiles over S - 1 for both, and so are the pieces.
 struct WholeOrBalanced {
     Walker cut;
     int32_t whole;  // this worker's sequence, -1: the balanced plan
     bool done;
     // All threads of the CTA call it; scratch and nthreads as for balanced_prepass.
-    __device__ void init_balanced(const int32_t* seqlens, int32_t B, int32_t S, int32_t w, int32_t W, int32_t slack, int32_t* scratch,
-                                  int nthreads) {
+    __device__ void init_balanced(const int32_t* seqlens, int32_t B, int32_t S, int32_t w, int32_t W, int32_t plan_W, int32_t slack,
+                                  int32_t* scratch, int nthreads) {
         const BalancedStart st = balanced_prepass(seqlens, B, S, w, W, scratch, nthreads);
         cut.init_balanced(seqlens, B, S, w, W, st);
         whole = -1;
         done = false;
-        if (B <= W && 2 * B > W) {
+        if (B <= plan_W && 2 * B > plan_W) {
             int32_t mx = 0;
             for (int32_t i = threadIdx.x & 31; i < B; i += 32) mx = max(mx, tiles_of(seqlens[i]));
             mx = __reduce_max_sync(0xffffffffu, mx);

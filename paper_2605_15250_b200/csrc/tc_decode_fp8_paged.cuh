@@ -48,6 +48,7 @@ struct Fp8PagedParams {
     int32_t hb, hshift;      // heads of a row block (a power of two) and its logarithm: row r is position r >> hshift, head r & (hb - 1)
     int32_t n_hb, row_blocks;  // row blocks over the heads; over heads and positions
     int32_t balanced, W;
+    int32_t plan_W, slack;   // of WholeOrBalanced
     int32_t n_rows, n_pages;
     float scale_log2;
     const __nv_bfloat16* q;  // [B, s_q, h_q, 576 or 192]
@@ -318,7 +319,7 @@ decode_fp8_paged_kernel(const Fp8PagedParams p, const __grid_constant__ CUtensor
     const int pq0 = rb / p.n_hb * (R >> p.hshift);      // first query position
     WholeOrBalanced walk;
     if (p.balanced) {
-        walk.init_balanced(p.seqlens, p.B, p.S, unit, p.W, LATENT ? 3 : 6, reinterpret_cast<int32_t*>(red), L::kThreads);
+        walk.init_balanced(p.seqlens, p.B, p.S, unit, p.W, p.plan_W, p.slack, reinterpret_cast<int32_t*>(red), L::kThreads);
     } else {
         walk.init_fixed(p.seqlens, p.B, p.S, unit / p.S, unit % p.S);
     }

@@ -30,6 +30,7 @@ namespace tc {
 struct Fp8PairParams {
     int32_t B, S, s_q, h_q, rows_total /* s_q*h_q */, row_blocks /* ceil(rows_total/128) */;
     int32_t balanced, W;  // balanced plan: W pairs per row block, grid = 2 * W * row_blocks
+    int32_t slack;        // of WholeOrBalanced
     int32_t n_rows, n_pages;
     float scale_log2;
     const __nv_bfloat16* q;   // [B, s_q * h_q, 576]
@@ -178,7 +179,7 @@ decode_fp8_pair_kernel(const Fp8PairParams p, const __grid_constant__ CUtensorMa
     const int rb = pair % p.row_blocks;
     WholeOrBalanced walk;
     if (p.balanced) {
-        walk.init_balanced(p.seqlens, p.B, p.S, pair / p.row_blocks, p.W, 6, reinterpret_cast<int32_t*>(sm_max), L::kThreads);
+        walk.init_balanced(p.seqlens, p.B, p.S, pair / p.row_blocks, p.W, p.W, p.slack, reinterpret_cast<int32_t*>(sm_max), L::kThreads);
     } else {
         const int unit = pair / p.row_blocks;
         walk.init_fixed(p.seqlens, p.B, p.S, unit / p.S, unit % p.S);
