@@ -272,8 +272,9 @@ gqla_status gqla_decode_gqa_fp8(const gqla_dims* dims, int32_t B, int32_t s_q, f
  * The paper writes k^R and q^R as they enter the scores, rotated; these calls take them as they leave their projections.
  * New rows come packed, sequence 0 first: row i (new_start[b] <= i < new_start[b+1]) of sequence b goes to position
  * t = seqlens[b] - new_start[b+1] + i, so that seqlens counts the new rows already and a step of s_q tokens has
- * new_start = 0, s_q, 2 s_q, ..; a prompt has as many rows as its sequence.  Rows at negative positions are skipped.
- * new_start int32 [B+1] (device, ascending, new_start[0] = 0, new_start[B] = n_new), seqlens int32 [B] (device).
+ * new_start = 0, s_q, 2 s_q, ..; a prompt has as many rows as its sequence.  Rows at negative positions are skipped, and so
+ * are rows from new_start[B] on (padding).
+ * new_start int32 [B+1] (device, ascending, new_start[0] = 0, new_start[B] <= n_new), seqlens int32 [B] (device).
  *   rope  fp32 [rope_rows, d_r]: row t holds the cosines of position t's d_r / 2 angles, then their sines.
  *   style GQLA_ROPE_PAIRS turns the columns (2 i, 2 i + 1), GQLA_ROPE_HALVES (i, i + d_r / 2), by angle i:
  *         (a, b) -> (a cos - b sin, a sin + b cos), in fp32, rounded once to what is stored.

@@ -31,7 +31,7 @@ struct NewRows {
     int64_t n;               // rows in all
     const int32_t* start;    // [B + 1]: sequence b's new rows are [start[b], start[b + 1])
     const int32_t* seqlens;  // [B], the new rows counted
-    // Sequence that owns new row i, and the row's position in it (negative: in front of the sequence, the row is skipped).
+    // Sequence that owns new row i (a row behind all of them: the last).
     __device__ __forceinline__ int32_t seq_of(int32_t i) const {
         int32_t lo = 0, hi = B - 1;
         while (lo < hi) {
@@ -41,7 +41,11 @@ struct NewRows {
         }
         return lo;
     }
-    __device__ __forceinline__ int32_t first_pos(int32_t b) const { return seqlens[b] - (start[b + 1] - start[b]); }
+    // The row's position in that sequence; negative where the row is skipped: in front of the sequence, or behind the last one's rows.
+    __device__ __forceinline__ int32_t pos_of(int32_t i, int32_t b) const {
+        const int32_t end = start[b + 1];
+        return i < end ? seqlens[b] - (end - i) : -1;
+    }
 };
 
 // Largest b in [0, B) with at(b) <= x, at ascending, at(0) <= x: a load per lane and round, 32-fold per round (a bisection is a chain of
@@ -193,7 +197,7 @@ __device__ __forceinline__ void rotate_queries(const NewRows& nr, const RopeTabl
     if (i >= nr.n * q.h_q * per) return;
     const int item = (int)(i % per), head = (int)(i / per % q.h_q);
     const int32_t tok = (int32_t)(i / per / q.h_q);
-    const int32_t b = nr.seq_of(tok), pos = nr.first_pos(b) + tok - nr.start[b];
+    const int32_t b = nr.seq_of(tok), pos = nr.pos_of(tok, b);
     if (pos < 0) return;
     if (pos >= rope.rows) return append_error(status, 1);
     RopeItem<VEC ? 8 : 1> x(rope, item);
@@ -287,7 +291,7 @@ __global__ void __launch_bounds__(kAppendThreads) append_rope_kernel(const Appen
     int32_t my_pos = 0;
     if (lane < n) {
         const int32_t tok = (int32_t)tok0 + lane, b = a.nr.seq_of(tok);
-        my_pos = a.nr.first_pos(b) + tok - a.nr.start[b];
+        my_pos = a.nr.pos_of(tok, b);
         if (my_pos >= a.rope.rows && a.rope.d_r > 0) append_error(a.status, 1);
         else if (my_pos >= 0) my_row = checked_row(a.rows, b, my_pos, a.cache_rows, a.status);
     }
@@ -423,7 +427,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kLatentThreads ? 3 : 16) a
     int32_t k;  // page of the sequence
     if (a.unit_shift < 0) {
         const int32_t pos = first + unit - s0;
-        if (pos < 0 || (unit != s0 && pos % page != 0)) return;
+        if (pos < 0 || pos >= T_len || (unit != s0 && pos % page != 0)) return;  // (T_len and on: rows behind the last sequence's)
         k = pos / page;
     } else {
         k = (first > 0 ? first / page : 0) + unit - ((s0 >> a.unit_shift) + 2 * b);
