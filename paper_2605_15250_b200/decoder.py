@@ -197,6 +197,12 @@ class GqlaFp8PagedDecoder(GqlaDecoder):
         if self.expanded != expanded:
             raise B.GqlaError("this decoder holds the %s" % ("GQA path's planes" if self.expanded else "absorb path's latent pages"))
 
+    def _rows(self, name: str, t: torch.Tensor, *shape: int) -> None:
+        """Refuses what the projections' calls, which go by these dimensions and the weights' type, would read or write out of bounds."""
+        if t.dtype != self.dtype or t.device != self.device or t.dim() != len(shape) + 1 or tuple(t.shape[1:]) != shape:
+            raise B.GqlaError(f"{name}: expected {self.dtype} [n, {', '.join(map(str, shape))}] on {self.device}, got {t.dtype} "
+                              f"{list(t.shape)} on {t.device}")
+
     def append(self, c: torch.Tensor, k_r: torch.Tensor, new_start: torch.Tensor, q_r: torch.Tensor | None = None):
         """The absorb path's new rows c [n, r_kv], k_r [n, d_r] (see GqlaDecoder.append); returns the rotated q_r."""
         self._need(False)
@@ -209,10 +215,11 @@ class GqlaFp8PagedDecoder(GqlaDecoder):
         """The GQA path's new rows: c [n, r_kv] is expanded (Sec. 3.1) and goes to the planes with the rotated k_r.  q [n, h_q,
         d_h + d_r]: the last d_r columns of the rows' queries are rotated in place."""
         self._need(True)
+        self._rows("c", c, self.r_kv)
         n = c.shape[0]
         k_c, v = (torch.empty((n, self.g, self.d_h), dtype=self.dtype, device=self.device) for _ in range(2))
-        # gqla_expand_cache wants rows at least r_kv + d_r apart, of which it reads the latent part where no k_r is asked for
-        if c.stride(0) < self.r_kv + self.d_r:
+        # gqla_expand_cache wants dense rows at least r_kv + d_r apart, of which it reads the latent part where no k_r is asked for
+        if c.stride(1) != 1 or c.stride(0) < self.r_kv + self.d_r:
             wide = torch.empty((n, self.r_kv + self.d_r), dtype=self.dtype, device=self.device)
             wide[:, :self.r_kv].copy_(c)
             c = wide
@@ -231,7 +238,11 @@ class GqlaFp8PagedDecoder(GqlaDecoder):
         """absorb_q -> decode_absorb_fp8_paged -> combine_up_proj, or with the merge in the decode call -> up_proj where many
         slots make that the faster one (GqlaDecoder.absorb_step)."""
         self._need(False)
-        Bn, s_q = q_c.shape[0], q_c.shape[1]
+        Bn, s_q = self.batch, q_c.shape[1] if q_c.dim() == 4 else 0
+        self._rows("q_c", q_c, s_q, self.h_q, self.d_h)
+        self._rows("q_r", q_r, s_q, self.h_q, self.d_r)
+        if q_c.shape[0] != Bn or q_r.shape[0] != Bn:
+            raise B.GqlaError(f"q_c, q_r: expected {Bn} sequences, got {q_c.shape[0]} and {q_r.shape[0]}")
         slots = abs(num_splits)
         q_hat = self._get("q_hat", (Bn, s_q, self.h_q, self.r_kv + self.d_r), self.dtype)
         o_part = self._get("o_part_a", (Bn, slots, s_q, self.h_q, self.r_kv), torch.float32)
