@@ -1,4 +1,4 @@
-"""NaN and infinities where they count: a NaN among what a query row attends makes that row NaN, and no other, through every
+"""NaN, infinities and scales at their ends where they count: a NaN among what a query row attends makes that row NaN, and no other, through every
 kernel and merge; none of them is ever taken for a row that sees nothing."""
 import math
 
@@ -8,6 +8,7 @@ import torch
 
 from paper_2605_15250_b200 import binding as B
 from paper_2605_15250_b200 import build as gbuild
+from tests.test_gpu_fp8_paged import _attend, _bounds
 
 pytestmark = pytest.mark.gpu
 
@@ -248,3 +249,55 @@ def test_huge_queries_are_no_infinities(kernel, splits):
     a.q = a.q * 2.0 ** 118
     big, big_lse = a.run(0.08 * 2.0 ** -118)
     assert torch.equal(big, out) and torch.equal(big_lse, lse)
+
+
+@pytest.mark.parametrize("kernel,splits", RUNS)
+@pytest.mark.parametrize("zeros", ["first", "last", "most"])
+def test_pages_of_the_smallest_scale_beside_ordinary_ones(kernel, splits, zeros):
+    """Pages of zeros as an append writes them (scale 2^-40), one of small codes at that scale and one of a large scale: a zero row
+    has a score of zero, which counts in full in the sum."""
+    a = Attention(kernel, splits)
+    for b, t in enumerate(LENS):
+        pages = [int(x) for x in a.table[b, :-(-t // PAGE)]]
+        empty = {"first": pages[:2], "last": pages[-2:], "most": pages[:3] + pages[5:]}[zeros]
+        for codes, scale in a.planes:
+            for page in empty:
+                codes[page * PAGE:(page + 1) * PAGE] = 0
+                scale[page] = 2.0 ** -40
+            if len(pages) > 4:
+                scale[pages[3]] = 2.0 ** -4
+                scale[pages[4]] = 2.0 ** -40
+    out, lse = a.run()
+    val = [c.cpu().view(torch.float8_e4m3fn).double().numpy() for c, _ in a.planes]
+    scl = [s.cpu().double().numpy() for _, s in a.planes]
+    heads = 1 if a.path == "absorb" else a.g
+    terms = "e5m2" if kernel == "pairs" else "e4m3"
+    for b, t in enumerate(LENS):
+        at = np.array([a.row(b, i) for i in range(t)], dtype=np.int64)
+        if t == 0:
+            assert not out[b].any() and bool(lse[b].isneginf().all())
+            continue
+        pg = at // PAGE
+        for j in range(heads):
+            per = a.h // heads
+            q = a.q[b, :, j * per:(j + 1) * per].cpu().double().numpy().reshape(S_Q * per, -1)
+            if a.path == "absorb":
+                k, v8, sv = val[0][at, 0] * scl[0][pg, :1], val[0][at, 0, :a.dv], scl[0][pg, 0]
+            else:
+                k = np.concatenate([val[0][at, j] * scl[0][pg, j][:, None], val[2][at, 0] * scl[2][pg]], axis=1)
+                v8, sv = val[1][at, j], scl[1][pg, j]
+            x = q @ k.T * 0.08
+            limits = [max(0, t - (S_Q - 1 - p)) for p in range(S_Q) for _ in range(per)]
+            o, l_ref, p = _attend(q, x, v8, sv, limits)
+            # fp32 sums of exact products, and query elements below 2^-15 of the row's largest, off by 2^-19 of it (as in that module)
+            width = q.shape[1]
+            x_err = 0.08 * float((np.abs(q) @ np.abs(k).T).max() * 2.0 ** -22 * math.sqrt(width)
+                                 + 2.0 ** -25 * np.abs(q).max() * np.abs(k).sum(1).max()) + 2.0 ** -21 * max(1.0, np.abs(x).max())
+            bound = _bounds(p, sv[None], v8, x_err, torch.finfo(a.q.dtype).eps / 2, terms)
+            got = out[b, :, j * per:(j + 1) * per].cpu().double().numpy().reshape(o.shape)
+            got_l = lse[b, :, j * per:(j + 1) * per].cpu().double().numpy().reshape(-1)
+            assert (np.abs(got - o) <= bound + 1e-30).all(), (b, j, float((np.abs(got - o) / (bound + 1e-30)).max()))
+            live = np.isfinite(l_ref)
+            assert np.array_equal(np.isfinite(got_l), live)
+            # (the kernels take exponents by the hardware's 2^x and logarithm, 2^-22 of a few tens in log2 units)
+            assert (np.abs(got_l[live] - l_ref[live]) <= x_err + 2.0 ** -16).all(), (b, j)
