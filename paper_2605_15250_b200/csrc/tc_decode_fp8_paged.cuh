@@ -34,7 +34,7 @@
 //   * The softmax warps read the query rows, cut them and write the swizzled operand themselves, at a piece's start.
 //   * Issuers and producer run converged (tc_common.cuh).
 #pragma once
-#include "append_rope.cuh"  // pow2_scale, bf16_max
+#include "append_rope.cuh"  // pow2_scale, bf16_finite_max
 #include "common.cuh"
 #include "sched.cuh"
 #include "tc_common.cuh"
@@ -170,7 +170,8 @@ __device__ __forceinline__ float rcp(float x) {
 }
 
 // Eight bf16 query elements times `inv` (a power of two: at most 448) as two codes each, hi (nearest) and lo (nearest to the rest).  By
-// way of fp16, which holds the eight bits of what is not below 2^-14.
+// way of fp16, which holds the eight bits of what is not below 2^-14.  Codes have no infinity: of an infinite element the rest gets 0 x
+// added, a NaN, as all scores of the row are then.
 __device__ __forceinline__ void split_query8(const uint4& u, float inv, uint2& hi, uint2& lo) {
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
     uint16_t h[4], l[4];
@@ -184,9 +185,10 @@ __device__ __forceinline__ void split_query8(const uint4& u, float inv, uint2& h
             "cvt.rn.satfinite.e4m3x2.f16x2 %0, h;\n\t"
             "cvt.rn.f16x2.e4m3x2 b, %0;\n\t"
             "sub.rn.f16x2 b, h, b;\n\t"
+            "fma.rn.f16x2 b, h, %4, b;\n\t"
             "cvt.rn.satfinite.e4m3x2.f16x2 %1, b;\n\t}"
             : "=&h"(h[i]), "=h"(l[i])
-            : "f"(x0), "f"(x1));
+            : "f"(x0), "f"(x1), "r"(0u));
     }
     hi = make_uint2((uint32_t)h[0] | ((uint32_t)h[1] << 16), (uint32_t)h[2] | ((uint32_t)h[3] << 16));
     lo = make_uint2((uint32_t)l[0] | ((uint32_t)l[1] << 16), (uint32_t)l[2] | ((uint32_t)l[3] << 16));
@@ -203,15 +205,16 @@ struct QueryPair {
             u[c] = valid && ci < kChunks ? reinterpret_cast<const uint4*>(row)[ci] : make_uint4(0, 0, 0, 0);
         }
     }
-    // Hands column 8 ci .. + 7's codes to store(first column, hi, lo); returns the row's scale, NaN for a row with an infinity.  sign: of
-    // the stored values.
+    // Hands column 8 ci .. + 7's codes to store(first column, hi, lo); returns the row's scale.  sign: of the stored values.
     template <typename F>
     __device__ __forceinline__ float cut(int lane, float sign, F store) const {
         uint32_t top = 0;
 #pragma unroll
         for (int c = 0; c < kPer; ++c) top = bf16_max(top, u[c]);
-        top &= 0x7fff7fffu;
-        float amax = __uint_as_float(max(top & 0xffffu, top >> 16) << 16);
+        float amax = bf16_finite_max(top, [&](auto f) {
+#pragma unroll
+            for (int c = 0; c < kPer; ++c) f(u[c]);
+        });
 #pragma unroll
         for (int o = 8; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
         const float qs = amax > 0.f ? pow2_scale(amax, -110) : 1.f;
@@ -223,8 +226,7 @@ struct QueryPair {
             split_query8(u[c], inv, hi, lo);
             if (ci < kChunks) store(ci * 8, hi, lo);
         }
-        // codes have no infinity: the scale makes a row's scores NaN (NaN elements, which amax may miss, are NaN codes)
-        return amax <= FLT_MAX ? qs : __uint_as_float(0x7fffffffu);
+        return qs;
     }
 };
 // OR of a predicate over the `nthreads` threads that call it on named barrier `id`.  (Warps that meet in barriers leave a loop by
