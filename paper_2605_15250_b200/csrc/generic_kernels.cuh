@@ -169,11 +169,19 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v) {
     u.y = *reinterpret_cast<uint32_t*>(&hi);
     *reinterpret_cast<uint2*>(p) = u;
 }
+// Coherent loads here and for the lse: the kernel in front still writes them when this one has been launched, which the read-only path
+// (ld.global.nc) does not allow.
+__device__ __forceinline__ float ld_lse(const float* p) {
+    float v;
+    asm volatile("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(p) : "memory");
+    return v;
+}
 __device__ __forceinline__ float4 ld_stream4(const float* p) {  // read once: do not keep in L1
     float4 v;
-    asm volatile("ld.global.nc.L1::no_allocate.v4.f32 {%0, %1, %2, %3}, [%4];"
+    asm volatile("ld.global.L1::no_allocate.v4.f32 {%0, %1, %2, %3}, [%4];"
                  : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-                 : "l"(p));
+                 : "l"(p)
+                 : "memory");
     return v;
 }
 template <typename TO, int V, int G>
@@ -217,11 +225,11 @@ __global__ void __launch_bounds__(kCombineThreads, 4) combine_vec_kernel(int64_t
         const int64_t b = (row0 + (have ? i : 0)) / rows_per_seq;
         const float* lp = lse_part + b * (S - 1) * rows_per_seq + row0 + (have ? i : 0);  // slot 0; + k * rows_per_seq
         float mx = -INFINITY;
-        for (int k = kl; k < S; k += span) mx = fmaxf(mx, __ldg(lp + (int64_t)k * rows_per_seq));
+        for (int k = kl; k < S; k += span) mx = fmaxf(mx, ld_lse(lp + (int64_t)k * rows_per_seq));
         for (int o = span >> 1; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
         float den = 0.f;
         for (int k = kl; k < S; k += span) {
-            const float e = slot_weight(__ldg(lp + (int64_t)k * rows_per_seq), mx);
+            const float e = slot_weight(ld_lse(lp + (int64_t)k * rows_per_seq), mx);
             den += e;
             if (have && k < kc) sw[i * kc + k] = e;
         }
@@ -243,7 +251,7 @@ __global__ void __launch_bounds__(kCombineThreads, 4) combine_vec_kernel(int64_t
                 const int row = i / kc, k = k0 + i % kc;
                 const int64_t bb = (row0 + row) / rows_per_seq;
                 const float mx = smax[row];
-                sw[i] = k < S ? slot_weight(__ldg(lse_part + (bb * (S - 1) + k) * rows_per_seq + row0 + row), mx) : 0.f;
+                sw[i] = k < S ? slot_weight(ld_lse(lse_part + (bb * (S - 1) + k) * rows_per_seq + row0 + row), mx) : 0.f;
             }
             __syncthreads();
         }

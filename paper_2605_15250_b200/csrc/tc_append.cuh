@@ -122,7 +122,8 @@ append_expand_tc_kernel(const AppendParams p, const __grid_constant__ CUtensorMa
         const int n16 = p.r_kv / 8;  // 16-byte pieces of a latent row
         // a row is n16 pieces; lane l copies pieces l and l + 32: piece cc is k-block cc / 8, 16-byte column
         // cc % 8 of that block's 128-byte row, XORed with the row's low three bits (the 128-byte swizzle)
-        // every load of the warp's 16 rows is issued before the first is used (the rows are cold in L2)
+        // every load of the warp's 16 rows is issued before the first is used (the rows are cold in L2); coherent ones, since the kernel
+        // in front (e.g. gqla_append_rope) still writes the rows when this one has been launched
         uint4 x[16][2], kr[16];
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
@@ -130,9 +131,9 @@ append_expand_tc_kernel(const AppendParams p, const __grid_constant__ CUtensorMa
             const uint4* src = reinterpret_cast<const uint4*>(p.cache + (n >= 0 ? n : 0) * p.cache_stride);
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-                x[r][h] = (n >= 0 && lane + 32 * h < n16) ? __ldg(src + lane + 32 * h) : make_uint4(0u, 0u, 0u, 0u);
+                x[r][h] = (n >= 0 && lane + 32 * h < n16) ? __ldcg(src + lane + 32 * h) : make_uint4(0u, 0u, 0u, 0u);
             // the shared RoPE key travels unchanged (one (plane, group) slice does it)
-            kr[r] = (p.k_r != nullptr && blockIdx.y == 0 && n >= 0 && lane < p.d_r / 8) ? __ldg(src + n16 + lane)
+            kr[r] = (p.k_r != nullptr && blockIdx.y == 0 && n >= 0 && lane < p.d_r / 8) ? __ldcg(src + n16 + lane)
                                                                                      : make_uint4(0u, 0u, 0u, 0u);
         }
 #pragma unroll

@@ -163,7 +163,7 @@ combine_up_tc_kernel(const CombineUpParams p, const __grid_constant__ CUtensorMa
 #pragma unroll
                 for (int i = 0; i < L::kMaxS / 8; ++i) {
                     const int k = k0 + 8 * i;
-                    v[i] = have && k < p.S ? __ldg(p.lse_part + pr + (int64_t)k * rows_per_seq) : -INFINITY;
+                    v[i] = have && k < p.S ? __ldcg(p.lse_part + pr + (int64_t)k * rows_per_seq) : -INFINITY;
                     M = fmaxf(M, v[i]);
                 }
 #pragma unroll
