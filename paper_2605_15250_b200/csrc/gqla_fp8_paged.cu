@@ -178,13 +178,13 @@ __global__ void __launch_bounds__(128) decode_fp8_paged_generic_kernel(const Fp8
     const int32_t lim = visible_limit(T, a.s_q, p);
     if (end > lim) end = lim;
     const TQ* q = (const TQ*)a.q + ((int64_t)(b * a.s_q + p) * a.h_q + i) * (a.dA + a.dB);
-    float finite = 0.f;  // NaN if an element of the query is no number or infinite: so are all scores of the row then, as on the tensor core
-    for (int d = lane; d < a.dA + a.dB; d += 32) finite = fmaf(ldf(q + d), 0.f, finite);
-    finite = warp_sum(finite);
+    float scale = 0.f;  // NaN if an element of the query is no number or infinite: so are all scores of the row then, as on the tensor core
+    for (int d = lane; d < a.dA + a.dB; d += 32) scale = fmaf(ldf(q + d), 0.f, scale);
+    scale = warp_sum(scale) + a.scale;
     float acc[kGenericCols];
 #pragma unroll
     for (int c = 0; c < kGenericCols; ++c) acc[c] = 0.f;
-    float m = -INFINITY, l = 0.f;
+    float m = -FLT_MAX, l = 0.f;  // (a score of -inf weighs nothing; a NaN, which fmaxf passes over, makes the sum NaN)
     int32_t page = -1;
     float sA = 1.f, sB = 0.f, sV = 1.f;
     for (int32_t s = begin; s < end; ++s) {
@@ -206,10 +206,10 @@ __global__ void __launch_bounds__(128) decode_fp8_paged_generic_kernel(const Fp8
         float dA = 0.f, dB = 0.f;
         for (int d = lane; d < a.dA; d += 32) dA = fmaf(ldf(q + d), ldf(ka + d), dA);
         for (int d = lane; d < a.dB; d += 32) dB = fmaf(ldf(q + a.dA + d), ldf(a.kB + n * a.kB_stride + d), dB);
-        const float x = fmaf(warp_sum(fmaf(dA, sA, dB * sB)), a.scale, finite);
+        const float x = warp_sum(fmaf(dA, sA, dB * sB)) * scale;
         const float m_new = fmaxf(m, x);
-        const float corr = m > -INFINITY ? expf(m - m_new) : 0.f;
-        const float e = m_new > -INFINITY || x != x ? expf(x - m_new) : 0.f;  // (fmaxf passes a NaN over: it makes the sum NaN)
+        const float corr = expf(m - m_new);
+        const float e = expf(x - m_new);
         l = l * corr + e;
         const float w = e * sV;
         const e4m3* vr = a.v + n * a.v_stride + (int64_t)j * a.dv;
