@@ -43,8 +43,8 @@ struct NewRows {
     }
     // The row's position in that sequence; negative where the row is skipped: in front of the sequence, or behind the last one's rows.
     __device__ __forceinline__ int32_t pos_of(int32_t i, int32_t b) const {
-        const int32_t end = start[b + 1];
-        return i < end ? seqlens[b] - (end - i) : -1;
+        const int32_t end = start[b + 1], T = seqlens[b];  // (both loads at once: a step waits for them)
+        return i < end ? T - (end - i) : -1;
     }
 };
 
