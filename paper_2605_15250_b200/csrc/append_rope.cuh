@@ -264,7 +264,7 @@ struct RowItems {
 };
 
 // A warp takes per_warp new rows: their places are looked up by a lane each, the latent parts copied eight 16-byte vectors a lane
-// at a time (49000 rows of 1152 bytes: 25.9 us, 5.3 TB/s; 41.7 with a block per sixteen rows and one vector a thread in flight), the RoPE parts rotated an
+// at a time (49000 rows of 1152 bytes: 26.5 us, 5.2 TB/s; 41.7 with a block per sixteen rows and one vector a thread in flight), the RoPE parts rotated an
 // item a lane.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kAppendThreads) append_rope_kernel(const AppendArgs a) {
@@ -399,8 +399,10 @@ struct AppendFp8Args {
 // The first sixteen chunks of a thread stay in its shared memory between the maximum and the coding: all of a page of 64 latent rows
 // with 256 threads, of 64 rows of one head of a plane with 64; larger pages read the rest again, from L1 or L2.  They come by
 // asynchronous copies, which cost no registers while they are on their way.  Few warps of many chunks, since looking the unit up costs
-// each warp some 400 instructions.  49000 latent rows and 20000 rows into the planes: 27.6 and 34.6 us (3.7 and 4.2 TB/s); twice the threads
-// with eight chunks each 31.4 and 39.0, those chunks in registers 40.0 and 43.4.
+// each warp some 400 instructions.  49000 latent rows and 20000 rows into the planes: 27.0 and 34.4 us in a graph (3.8 and 4.2 TB/s); twice
+// the threads with eight chunks each 31.4 and 39.0, those chunks in registers 40.0 and 43.4.  Pages of 16, 32, 128 and 256 rows: 41.4, 28.4,
+// 47.8 and 65.2 us, planes 60.9, 39.7, 48.5 and 74.6 -- small pages have a look-up for few rows, large ones read twice what is not held and
+// have fewer blocks.  fp32 rows are not held either: 56.8 and 64.9.
 constexpr int kLatentThreads = 256, kPlaneThreads = 64;
 template <typename T, bool VEC, int THREADS>
 struct HeldChunks {

@@ -146,7 +146,9 @@ struct Fp8PagedCall {
     bool latent;
 };
 
-// Any dimensions, any page size, bf16 or fp32 queries: one warp per (sequence, split, position, head) row, fp32 throughout.
+// Any dimensions, any page size, bf16 or fp32 queries: one warp per (sequence, split, position, head) row, fp32 throughout.  Bound by its
+// instructions, a load and a decoding per code and head: 8 x 1024 rows, 32 heads, eight splits, fp32 queries 290 us on the absorb path, 221 on
+// the GQA path.
 struct Fp8PagedGeneric {
     const void* q;
     const e4m3 *kA, *kB, *v;
@@ -256,8 +258,9 @@ bool covers(const gqla_dims& d, gqla_dtype dtype, int32_t s_q, int32_t page_size
            page_size % 16 == 0 && s_q <= 4096;
 }
 
-// Absorb path: CTA pairs with the query rows on M beyond 64 rows.  64 sequences of 4096 rows: 64 heads 66 us on the
-// tokens-on-M kernel and 80 on pairs, half of whose rows are empty then; 128 heads 115 and 77.
+// Absorb path: CTA pairs with the query rows on M beyond 64 rows.  64 sequences of 4096 rows in a graph, on the tokens-on-M kernel and on
+// pairs: 64 heads 66 and 80 us (half of a pair's rows are empty then), 72 heads 89 and 72, 40 heads at s_q = 2 110 and 73, 28 at 3 91 and
+// 73, 32 at 3 93 and 74, 128 heads 115 and 77; 128 ragged ones of 256 to 4096 rows, 72 heads 125 and 112.
 bool on_pairs(const gqla_dims& d, int32_t s_q, bool latent) { return latent && (int64_t)s_q * d.h_q > 64; }
 
 // CTA pairs resident at once on the current device, 0 where it cannot be asked.
@@ -309,7 +312,10 @@ bool few_pieces(const Fp8PagedCall& c) {
     return pieces <= std::min(token_workers(*c.d, c.s_q, c.latent), c.S < 0 ? workers_of(*c.d, c.s_q, c.latent) : 0x7fffffff);
 }
 
-// Tiles by which the longest sequence may exceed a share for every sequence to be one piece.
+// Tiles by which the longest sequence may exceed a share for every sequence to be one piece.  Equal sequences of m tiles, cut and whole, us
+// in a graph: absorb path, 100 of 32 heads (an excess of 0.32 m) m = 4 28.4 and 23.2, 9 36.3 and 31.5, 20 50.4 and 48.3; 50 of 128
+// heads on pairs (also 0.32 m) 4 37.0 and 27.8, 18 56.0 and 50.3, 24 63.0 and 60.2, 32 71.7 and 72.6; GQA path, 14 of 32 heads (0.22 m)
+// 8 19.0 and 15.4, 24 28.4 and 26.9, 32 32.8 and 32.1, 48 42.0 and 42.5.  With the excess at its bound, that is, whole sequences still win.
 int32_t whole_slack(const gqla_dims& d, int32_t s_q, bool latent) { return latent && !on_pairs(d, s_q, latent) ? 3 : 6; }
 
 template <int R, bool LATENT, int PG>
@@ -488,7 +494,8 @@ gqla_status gqla_append_rope(const gqla_dims* d, gqla_dtype dtype, int32_t B, in
     a.rows = block_table != nullptr ? RowMap{nullptr, block_table, max_pages, page_size} : RowMap{seq_start, nullptr, 0, 1};
     a.status = status_word;
     // a row per warp while that does not fill the GPU, four beyond (each lane then keeps eight loads of a latent part of 1 KB in
-    // flight; eight rows: 12000 8.3 against 7.8 us, 39000 20.3 against 19.8, 98000 40.9 against 41.3)
+    // flight).  One and four rows a warp, in a graph: 4000 rows 4.7 and 5.4 us, 6000 6.9 and 4.8, 8192 8.3 and 7.1, 12000 11.4 and 8.0, 16000
+    // 15.6 and 9.0 (eight: 12000 8.3, 39000 20.3 against 19.8 with four, 98000 40.9 against 41.3)
     a.per_warp = n_new >= 8192 ? kAppendMostRows : 1;
     const int64_t rows_per_block = (int64_t)a.per_warp * (kAppendThreads / 32);
     const int64_t kv = (n_new + rows_per_block - 1) / rows_per_block;

@@ -25,9 +25,12 @@
 //   * R = 16 or 32 query rows per CTA.  More rows (64 heads of the absorb path, s_q > 1) are blocks of 32 on CTAs of their own
 //     that walk the same tiles at the same time, so that the cache comes from HBM once and from L2 otherwise.  (Beyond 64 rows
 //     absorb path calls of more pieces than workers here run on tc_decode_fp8_pair.cuh.)
-//   * Measured, merge included.  Absorb path, 32 heads, 128 ragged sequences of up to 16384 rows: 127 us, 4.5 TB/s.  GQA path: 32 heads, 64
-//     of up to 16384, 206 us, 5.5 TB/s, bound by HBM; 128 heads, s_q = 2, 64 of 4096, 131 us, 4.3 TB/s, bound by the softmax warps' issue
-//     slots (32 rows x 128 tokens a tile on one SM) and by what they wait for.
+//   * Measured, merge included, in a graph of 18 passes; in brackets calls one after another for longer, at the power cap.  Absorb path, 32
+//     heads, 128 ragged sequences of up to 16384 rows: 127 us, 4.5 TB/s (142 to 149).  GQA path: 32 heads, 64 of up to 16384, 207 us, 5.5
+//     TB/s, bound by HBM (213 to 224); 128 heads, s_q = 2, 64 of 4096, 130 us, 4.3 TB/s (143 to 150), with 45 % of the issue slots, 47 % of
+//     DRAM and 13 % of the tensor pipe in use: bound by a tile's chain of waits (scores -> maximum -> weights -> P V).  In the same way the
+//     absorb path's tile (25 %, 38 % and 16 %).  A chunk of 256 query positions over 2 x 4096 rows, 32 heads: absorb path 136 us on pairs
+//     (1.08 PFLOP/s of the method's products), GQA path 146 us (0.29).
 //   * Absorb path: V is the latent part of the K tile, which is read in both orders from one place in shared memory.
 //   * Tiles are fetched in boxes of PG rows, the largest of 64, 32 or 16 that divides the page.  What lies behind a sequence's end in its last
 //     page may be anything, NaN codes included: scores are selected by position, V rows are zeros there (CutMaps).

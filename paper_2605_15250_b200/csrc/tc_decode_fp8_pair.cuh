@@ -6,7 +6,7 @@
 //
 // Bound by the tensor core and by a piece's ends: a tile's MMAs take about 2540 cycles back to back and a tile 2650
 // to 2800 (tensor pipe active 56 % of the SM's cycles); a piece costs another 18000 (queries 6000, first references 5000, output 7000).  128 heads, 64 x 4096 rows:
-// 77 us merge included, 0.95 PFLOP/s of the method's products, each done twice here.
+// 76 us merge included in a graph of 18 passes, 0.96 PFLOP/s of the method's products, each done twice here; 90 to 92 at the power cap.
 //
 //   * Queries: hi and lo, both E4M3, written to shared memory by the softmax warps at a piece's start; S = (Q_hi + Q_lo) K^T in one
 //     accumulator, 36 MMAs a tile.
