@@ -9,9 +9,12 @@ from __future__ import annotations
 
 import ctypes
 import os
+import sys
 from ctypes import c_char_p, c_float, c_int32, c_int64, c_void_p
 
 import torch
+
+from . import build
 
 _PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 # GQLA_LIB_PATH selects another build of the same library (e.g. the -DGQLA_DEBUG one, libgqla_debug.so)
@@ -458,12 +461,13 @@ def _marshal():
     """The module that checks these calls' tensors and makes them (marshal.cpp).  Built along with libgqla.so."""
     global _marshal_module
     if _marshal_module is None:
+        if os.path.exists(build.MARSHAL_PATH) and not build.marshal_fits():  # (looked at before it is loaded)
+            raise GqlaError(f"{build.MARSHAL_PATH} was built for another torch or Python than {torch.__version__} and "
+                            f"{sys.version.split()[0]}: build it again with `python -m paper_2605_15250_b200.build`")
         try:
             from . import _marshal as module
         except ImportError as e:
             raise GqlaError(f"{e}: build it with `python -m paper_2605_15250_b200.build`") from e
-        if module.built_for.split("+")[0] != torch.__version__.split("+")[0]:
-            raise GqlaError(f"_marshal.so was built for torch {module.built_for}, this is {torch.__version__}: build it again")
         names = ("gqla_append_rope", "gqla_append_rope_fp8", "gqla_append_planes_fp8", "gqla_decode_absorb_fp8_paged",
                  "gqla_decode_gqa_fp8_paged", "gqla_status_str")
         module.bind(GqlaError, *(ctypes.cast(getattr(lib(), name), c_void_p).value for name in names))

@@ -38,11 +38,14 @@ def _marshal_stamp() -> bytes:
     return f"built for torch {importlib.metadata.version('torch').split('+')[0]}, Python {sys.version_info[0]}.{sys.version_info[1]};".encode()
 
 
-def _marshal_is_current(sources: list[str]) -> bool:
-    if not os.path.exists(MARSHAL_PATH) or os.path.getmtime(MARSHAL_PATH) < max(os.path.getmtime(f) for f in sources):
-        return False
+def marshal_fits() -> bool:
+    """Whether the extension that is there was compiled for this torch and Python."""
     with open(MARSHAL_PATH, "rb") as f:
         return _marshal_stamp() in f.read()
+
+
+def _marshal_is_current(sources: list[str]) -> bool:
+    return os.path.exists(MARSHAL_PATH) and os.path.getmtime(MARSHAL_PATH) >= max(os.path.getmtime(f) for f in sources) and marshal_fits()
 
 
 def build_marshal(force: bool = False) -> str:

@@ -389,12 +389,12 @@ PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, kMethods,
 
 #define TEXT_OF(x) #x
 #define TEXT(x) TEXT_OF(x)
-// (build.py looks for this in the file)
+// (build.py and the binding look for this in the file)
 constexpr char kStamp[] = "built for torch " TORCH_VERSION ", Python " TEXT(PY_MAJOR_VERSION) "." TEXT(PY_MINOR_VERSION) ";";
 
 PyMODINIT_FUNC PyInit__marshal() {
     PyObject* m = PyModule_Create(&kModule);
-    if (m != nullptr && (PyModule_AddStringConstant(m, "built_for", TORCH_VERSION) != 0 || PyModule_AddStringConstant(m, "stamp", kStamp) != 0)) {
+    if (m != nullptr && PyModule_AddStringConstant(m, "stamp", kStamp) != 0) {
         Py_DECREF(m);
         return nullptr;
     }

@@ -51,6 +51,17 @@ def test_the_extension_that_is_built_carries_the_stamp():
         assert gbuild._marshal_stamp() in f.read()
 
 
+def test_extension_of_another_torch_or_python_is_not_loaded(monkeypatch, tmp_path):
+    from paper_2605_15250_b200 import binding as B
+
+    other = tmp_path / "_marshal.so"
+    other.write_bytes(b"built for torch 1.0.0, Python 3.12;")
+    monkeypatch.setattr(gbuild, "MARSHAL_PATH", str(other))
+    monkeypatch.setattr(B, "_marshal_module", None)
+    with pytest.raises(B.GqlaError, match="another torch or Python.*build it again"):
+        B._marshal()
+
+
 def test_library_comes_first_and_alone_without_torch(compilers, monkeypatch):
     gbuild.build()
     assert [os.path.basename(c[c.index("-o") + 1]).split(".so")[0] for c in compilers] == ["libgqla", "_marshal"]
