@@ -333,10 +333,11 @@ gqla_status gqla_append_planes_fp8(const gqla_dims* dims, gqla_dtype dtype, int3
  * each query and each probability, which keep as much (a query element below 2^-15 of its row's largest keeps an
  * absolute error of 2^-19 of that one; a probability 2^-9 of itself, 2^-8 on the absorb path with s_q * h_q > 64 and many pieces, and
  * 2^-20 of its row's largest).  Rows of a sequence's last page behind its end may hold anything.
- * NaN: a query row that holds one or an infinity, or that sees a key row with a NaN code (absorb path: anywhere in the row; GQA path: K_C of
- * its group or k_R), gets out and lse NaN, also through the merges; a NaN code in V makes its column of out NaN.  What a row
- * does not see leaves its lse alone; on the tensor-core kernels a NaN in the values of one of the step's own rows may reach
- * the same column of out at the step's earlier positions.
+ * NaN: a query row that holds one or an infinity, or that sees a key row with a NaN code (absorb path: anywhere in the row;
+ * GQA path: in K_C of its group or in k_R), gets out and lse NaN, also through the merges; a NaN code in V makes its column
+ * of out NaN.  A row that sees nothing has out = 0 and lse = -inf whatever its query holds.  What a row does not see leaves
+ * its lse alone; on the tensor-core kernels a NaN among the values of one of the step's own rows may reach the same column
+ * of out at the step's earlier positions.
  * Block table, lengths, splits (num_splits >= 1 fixed plan, <= -2 balanced), partials and status word as for
  * gqla_decode_absorb_paged / gqla_decode_gqa_paged; with `out` not NULL ([B, s_q, h_q, r_kv] or [.., d_h] of `dtype`) the call
  * also merges the partials as gqla_combine_splits does (lse fp32 [B, s_q, h_q] or NULL, NULL without out).  Tensor-core kernels:

@@ -488,7 +488,8 @@ def gqla_append_rope(dims: GqlaDims, c: torch.Tensor, k_r: torch.Tensor, new_sta
                      q_out: torch.Tensor | None = None, status_word: torch.Tensor | None = None) -> None:
     """Writes the new rows [c ; rotated k_r] to the latent cache [N, r_kv+d_r] (packed: seq_start; paged: block_table and
     page_size) and rotates their queries q_r [n, h_q, d_r] into q_out.  c [n, r_kv], k_r [n, d_r]: packed over the
-    sequences, sequence b's rows are new_start[b]..new_start[b+1] (int32 [B+1]) and end at position seqlens[b] - 1.
+    sequences, sequence b's rows are new_start[b]..new_start[b+1] (int32 [B+1]) and end at position seqlens[b] - 1; rows from
+    new_start[B] on are padding and left out.
     rope fp32 [positions, d_r] = [cosines ; sines]; style "pairs" (2i, 2i+1) or "halves" (i, i + d_r/2)."""
     (_marshal_module or _marshal()).gqla_append_rope(dims, c, new_start, seqlens, rope, _style(style), k_r, q_r, q_out, cache, seq_start,
                                                      block_table, page_size, status_word)

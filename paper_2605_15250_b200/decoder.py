@@ -69,7 +69,8 @@ class GqlaDecoder:
     def append(self, c: torch.Tensor, k_r: torch.Tensor, new_start: torch.Tensor, rope: torch.Tensor, style: str = "pairs",
                q_r: torch.Tensor | None = None) -> torch.Tensor | None:
         """Writes a step's or a prompt's rows [c ; rotated k_r] to the latent cache (seqlens already counts them; packed rows,
-        sequence b's are new_start[b]..new_start[b+1]) and returns their queries q_r [n, h_q, d_r] rotated."""
+        sequence b's are new_start[b]..new_start[b+1], and rows from new_start[B] on are padding) and returns their queries
+        q_r [n, h_q, d_r] rotated."""
         q_out = None if q_r is None else torch.empty(q_r.shape, dtype=q_r.dtype, device=self.device)
         B.gqla_append_rope(self.dims, c, k_r, new_start, self.seqlens, rope, style, self.cache,
                            None if self.block_table is not None else self.seq_start, self.block_table, self.page_size, q_r, q_out,
@@ -145,7 +146,8 @@ class GqlaDecoder:
         """Captures one call of `step` (absorb_step or gqa_step) with these argument tensors into a CUDA
         graph and returns (replay, output).  The step reads its inputs from the SAME tensors on every
         replay (copy new queries into them first) and writes the same output tensors.  All buffers are
-        allocated during the warm-up calls, so nothing is allocated while capturing."""
+        allocated during the warm-up calls, so nothing is allocated while capturing.  Graphs and eager calls of one
+        decoder share its buffers: run them on one stream, or one after another."""
         side = torch.cuda.Stream(device=self.device)
         side.wait_stream(torch.cuda.current_stream())
         with torch.cuda.stream(side):
